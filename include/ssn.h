@@ -462,6 +462,143 @@ ssn_status_t ssn_sparta_average(int64_t R, int64_t m, const float *const *chunks
 ssn_status_t ssn_delta_rule(int64_t n, int64_t m, const int64_t *I, int64_t first, float *theta,
                             const float *avg, const float *snap, float lambda, void *stream);
 
+/*
+ * The attention sublayer of a stage (section 5.2's model: grouped queries,
+ * norms of queries and keys for each head, rotary positions), between the
+ * codec's decompress and the output projection that ssn_reparam_forward adds
+ * to the residual stream: norms and rotation for training, the same on the
+ * way into a paged cache for serving, and attention over that cache.
+ *
+ * Rows of heads: a tensor [N, H, D] is given by its pointer and its row
+ * stride `ld` in elements (ld >= H * D), the heads of a row packed, so that
+ * queries, keys and values may be parts of one [N, ld] projection.  Outputs
+ * may be parts of one buffer as well; they must not overlap inputs or each
+ * other.  The kernels' fast paths need D = 64, 128 or 256, 16-byte aligned
+ * pointers and row strides of a multiple of 16 bytes; other shapes (D <= 1024,
+ * else SSN_ERR_UNSUPPORTED) run the generic kernels.
+ *
+ * Rotation: `table` [P, R] float32 holds in row p the R / 2 cosines and then
+ * the R / 2 sines of position p; R is even, 0 <= R <= D (0: no rotation, the
+ * table may be NULL), and elements R .. D-1 of a head pass as they are.
+ * SSN_ROPE_HALVES turns the pairs (i, i + R/2), SSN_ROPE_PAIRS (2i, 2i + 1).
+ * Positions outside [0, P) are a contract violation: they are clamped.
+ *
+ * Norm: eps >= 0 divides a head by sqrt(mean(x^2) + eps) and multiplies it by
+ * the weight w [D] (dtype; NULL: ones); eps < 0: no norm, w must be NULL.
+ * All of it is computed in float32 and rounded once.
+ */
+typedef enum { SSN_ROPE_HALVES = 0, SSN_ROPE_PAIRS = 1 } ssn_rope_t;
+
+/*
+ * ssn_rope_table -- table[p, i] = cos(p theta^(-2i/R)) and table[p, R/2 + i] =
+ * sin(p theta^(-2i/R)) for p in [0, P), i in [0, R/2), in float64 and rounded
+ * once.  theta > 0 and finite; R even.  Made once per run.
+ */
+ssn_status_t ssn_rope_table(int64_t P, int64_t R, double theta, float *table, void *stream);
+
+/*
+ * ssn_qk_norm_rope -- norm and rotation of queries [N, Hq, D] and keys
+ * [N, Hk, D] in one launch: Out = rot_pos(norm(In)).  Hq or Hk may be 0 (its
+ * pointers are then not looked at).  pos [N] int32 (may be NULL if R == 0).
+ */
+ssn_status_t ssn_qk_norm_rope(ssn_dtype_t dtype, int64_t N, int64_t Hq, int64_t Hk, int64_t D,
+                              int64_t R, int64_t P, ssn_rope_t style, float eps, const void *Q,
+                              int64_t ldq, const void *K, int64_t ldk, const void *wq,
+                              const void *wk, const int32_t *pos, const float *table, void *Qout,
+                              int64_t ldqo, void *Kout, int64_t ldko, void *stream);
+
+/*
+ * ssn_qk_norm_rope_backward -- its gradients, for GQ = dL/dQout and GK:
+ *   GQin [N, Hq, D], GKin [N, Hk, D]  dtype    dL/dQ, dL/dK
+ *   Gwq, Gwk [D]                      float32  dL/dw, summed over tokens and
+ *                                     heads (NULL: not wanted; NULL without norm)
+ * Q and K are the forward's inputs.  The weight gradients are summed by
+ * blocks into `workspace` (device, 4-byte aligned, at least
+ * ssn_qk_norm_rope_workspace_bytes, else SSN_ERR_SHAPE; NULL if neither is
+ * wanted) and then in block order: repeated calls give the same bits.  N == 0
+ * sets them to zero.
+ */
+size_t ssn_qk_norm_rope_workspace_bytes(ssn_dtype_t dtype, int64_t N, int64_t Hq, int64_t Hk,
+                                        int64_t D);
+ssn_status_t ssn_qk_norm_rope_backward(ssn_dtype_t dtype, int64_t N, int64_t Hq, int64_t Hk,
+                                       int64_t D, int64_t R, int64_t P, ssn_rope_t style, float eps,
+                                       const void *Q, int64_t ldq, const void *K, int64_t ldk,
+                                       const void *wq, const void *wk, const int32_t *pos,
+                                       const float *table, const void *GQ, int64_t ldgq,
+                                       const void *GK, int64_t ldgk, void *GQin, int64_t ldgqi,
+                                       void *GKin, int64_t ldgki, float *Gwq, float *Gwk,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A batch of sequences over a paged cache, all on the device:
+ *   Kc, Vc [npages, Hk, page_size, D] dtype  the cache; any page size
+ *   pages  [B, width] int32   pages[b, j] holds positions j * page_size .. of
+ *                             sequence b; entries past a sequence's last page
+ *                             are not read
+ *   starts [B + 1] int32      sequence b has the new tokens starts[b] ..
+ *                             starts[b + 1] - 1 of the N rows (ascending;
+ *                             none is fine; rows from starts[B] on are padding)
+ *   lens   [B] int32          its length, the new tokens included: row i of it
+ *                             has position lens[b] - (starts[b + 1] - i)
+ * A captured graph may be replayed with other contents.  Out-of-range entries
+ * are a contract violation: page numbers, row ranges and lengths are clamped
+ * (to npages, N, width * page_size and, in the attention, max_len), so memory
+ * stays in bounds, and the results are unspecified.  width * page_size,
+ * N * Hq and npages * Hk * page_size stay below 2^31, and B below 2^20.
+ */
+
+/*
+ * ssn_kv_append -- the serving form of ssn_qk_norm_rope, one launch: for the
+ * row i of sequence b at position p,
+ *   Kc[pages[b, p / page_size], h, p % page_size, :] = rot_p(norm(K[i, h, :]))
+ *   Vc[pages[b, p / page_size], h, p % page_size, :] = V[i, h, :]
+ *   Qout[i, h, :] = rot_p(norm(Q[i, h, :]))      (Hq == 0: no queries)
+ * Nothing else of the cache is touched.  Rows with a negative position (a
+ * length below the number of new tokens) write nothing, nor does padding.  No
+ * two rows may share a cache slot.
+ */
+ssn_status_t ssn_kv_append(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk,
+                           int64_t D, int64_t R, int64_t P, ssn_rope_t style, float eps,
+                           const void *Q, int64_t ldq, const void *K, int64_t ldk, const void *V,
+                           int64_t ldv, const void *wq, const void *wk, const float *table,
+                           void *Kc, void *Vc, int64_t npages, int64_t page_size,
+                           const int32_t *pages, int64_t width, const int32_t *starts,
+                           const int32_t *lens, void *Qout, int64_t ldqo, void *stream);
+
+/*
+ * ssn_paged_attention -- attention of the new tokens over the cache, which
+ * holds their keys and values already: the row i at position p of sequence b
+ * sees positions 0 .. p,
+ *   O[i, h, :] = sum_t softmax_t(scale Q[i, h, :] . K_t) V_t
+ * with key head h / (Hq / Hk); Hq is a multiple of Hk.  A row that sees
+ * nothing (a negative position) gives zeros and lse -inf; padding is not
+ * written.  What the cache holds in positions a row does not see has no
+ * effect on it, whatever it is.
+ *   max_q, max_len  host bounds on a sequence's new tokens and length; they
+ *                   choose the launch shape
+ *   O [N, Hq, D] dtype;  lse [N, Hq] float32 or NULL: the natural logarithm of
+ *                   sum_t exp(scale Q . K_t)
+ *   workspace       16-byte aligned device memory, any contents: where rows
+ *                   are few the keys are split into ranges whose partial
+ *                   results (float32) are joined in order.
+ *                   ssn_paged_attention_workspace_bytes is the size that
+ *                   allows every split; a smaller one (or NULL with 0 bytes)
+ *                   allows fewer or none.
+ * Products of bf16 storage are matrix-core products with float32 sums; the
+ * probabilities are rounded to bf16 for the product with V, their sum is not.
+ * Float32 storage is computed in float32 throughout.  Repeated calls give the
+ * same bits.
+ */
+size_t ssn_paged_attention_workspace_bytes(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq,
+                                           int64_t Hk, int64_t D, int64_t max_q, int64_t max_len);
+ssn_status_t ssn_paged_attention(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk,
+                                 int64_t D, int64_t max_q, int64_t max_len, float scale,
+                                 const void *Q, int64_t ldq, const void *Kc, const void *Vc,
+                                 int64_t npages, int64_t page_size, const int32_t *pages,
+                                 int64_t width, const int32_t *starts, const int32_t *lens, void *O,
+                                 int64_t ldo, float *lse, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
 #ifdef __cplusplus
 }
 #endif

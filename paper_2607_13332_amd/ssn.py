@@ -110,6 +110,26 @@ def _declare(lib):
     lib.ssn_project_weights_batched.argtypes = [ctypes.c_int, _c_i64, _c_i64,
                                                 ctypes.POINTER(_c_i64), _c_i64,
                                                 ctypes.POINTER(_c_p), _c_p, _c_p]
+    _sz = ctypes.c_size_t
+    lib.ssn_rope_table.restype = ctypes.c_int
+    lib.ssn_rope_table.argtypes = [_c_i64, _c_i64, ctypes.c_double, _c_p, _c_p]
+    heads = [ctypes.c_int] + [_c_i64] * 6 + [ctypes.c_int, ctypes.c_float]      # dtype .. eps
+    lib.ssn_qk_norm_rope.restype = ctypes.c_int
+    lib.ssn_qk_norm_rope.argtypes = heads + [_c_p, _c_i64] * 2 + [_c_p] * 4 + [_c_p, _c_i64] * 2 + [_c_p]
+    lib.ssn_qk_norm_rope_workspace_bytes.restype = _sz
+    lib.ssn_qk_norm_rope_workspace_bytes.argtypes = [ctypes.c_int] + [_c_i64] * 4
+    lib.ssn_qk_norm_rope_backward.restype = ctypes.c_int
+    lib.ssn_qk_norm_rope_backward.argtypes = heads + [_c_p, _c_i64] * 2 + [_c_p] * 4 + \
+        [_c_p, _c_i64] * 4 + [_c_p] * 3 + [_sz, _c_p]
+    paged = [_c_p, _c_p, _c_i64, _c_i64, _c_p, _c_i64, _c_p, _c_p]               # Kc .. lens
+    lib.ssn_kv_append.restype = ctypes.c_int
+    lib.ssn_kv_append.argtypes = [ctypes.c_int] + [_c_i64] * 7 + [ctypes.c_int, ctypes.c_float] + \
+        [_c_p, _c_i64] * 3 + [_c_p] * 3 + paged + [_c_p, _c_i64, _c_p]
+    lib.ssn_paged_attention_workspace_bytes.restype = _sz
+    lib.ssn_paged_attention_workspace_bytes.argtypes = [ctypes.c_int] + [_c_i64] * 7
+    lib.ssn_paged_attention.restype = ctypes.c_int
+    lib.ssn_paged_attention.argtypes = [ctypes.c_int] + [_c_i64] * 7 + [ctypes.c_float, _c_p, _c_i64] + \
+        paged + [_c_p, _c_i64, _c_p, _c_p, _sz, _c_p]
     return lib
 
 
@@ -616,3 +636,225 @@ def delta_rule(theta: torch.Tensor, avg: torch.Tensor, snap: Optional[torch.Tens
         _dev(avg, "avg", torch.float32, 1),
         0 if snap is None else _dev(snap, "snap", torch.float32, 1), float(lam), _stream(stream)))
     return theta
+
+
+# --------------------------------------------------------------------------
+# The attention sublayer between decompress and the output projection: norms
+# of heads with the position rotation, a paged cache, attention over it.
+# Tensors of heads are [N, H, D] with packed heads and any row stride (parts of
+# one projection); the cache is [pages, Hk, page_size, D].
+# --------------------------------------------------------------------------
+ROPE_STYLES = {"halves": 0, "pairs": 1}
+
+
+def _rows(t: torch.Tensor, name: str, first: torch.Tensor, dev: int, dtype, shape) -> tuple:
+    """(data_ptr, row stride) of a tensor [N, H, D] on the GPU `dev` of the
+    call's `first` tensor, heads of a row packed."""
+    if t.get_device() != dev or t.dtype != dtype or dev < 0:
+        _same_device(first, t)
+        if dev < 0 or not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor (the codec has no CPU path)")
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    N, H, D = shape
+    ld, sh, se = t.stride()
+    if (se != 1 and D > 1) or (sh != D and H > 1) or (ld < H * D and N > 1):
+        raise ValueError(f"the heads of a row of {name} must be contiguous, got strides {t.stride()}")
+    return t.data_ptr(), (ld if N > 1 else H * D)
+
+
+def _rotation(table, style, eps, D, wq, wk):
+    """(P, R, style code, eps) of a call's norm and rotation."""
+    if style not in ROPE_STYLES:
+        raise ValueError(f"style must be one of {tuple(ROPE_STYLES)}, got {style!r}")
+    if eps is None and (wq is not None or wk is not None):
+        raise ValueError("weights without a norm (eps is None)")
+    P, R = (1, 0) if table is None else table.shape
+    return P, R, ROPE_STYLES[style], (-1.0 if eps is None else float(eps))
+
+
+def _weight(w, name, first, dev, dtype, D):
+    if w is None:
+        return None
+    if w.shape != (D,):
+        raise ValueError(f"{name} has shape {tuple(w.shape)}, expected ({D},)")
+    return _gpu(w, name, first, dev, dtype, 1)
+
+
+def rope_table(P: int, R: int, theta: float = 10000.0, device=None,
+               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The rotation table float32 [P, R] of positions 0 .. P-1: R / 2 cosines,
+    then R / 2 sines of p theta^(-2i/R), made once per run."""
+    if out is None:
+        out = torch.empty((P, R), dtype=torch.float32, device="cuda" if device is None else device)
+    if out.shape != (P, R):
+        raise ValueError(f"out has shape {tuple(out.shape)}, expected ({P}, {R})")
+    _check("ssn_rope_table", lib().ssn_rope_table(P, R, float(theta), _dev(out, "out", torch.float32, 2),
+                                                  _stream(stream)))
+    return out
+
+
+def qk_norm_rope(Q: torch.Tensor, K: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                 table: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None,
+                 wk: Optional[torch.Tensor] = None, eps: Optional[float] = 1e-6,
+                 style: str = "halves", Qout: Optional[torch.Tensor] = None,
+                 Kout: Optional[torch.Tensor] = None, stream=None):
+    """Queries [N, Hq, D] and keys [N, Hk, D], each head divided by its root
+    mean square (eps None: no norm), times wq / wk [D], and rotated to its
+    position (table None: not rotated).  Returns (Qout, Kout)."""
+    N, Hq, D = Q.shape
+    Hk = K.shape[1]
+    P, R, code, e = _rotation(table, style, eps, D, wq, wk)
+    t, g = Q.dtype, Q.get_device()
+    if Qout is None:
+        Qout = torch.empty((N, Hq, D), dtype=t, device=Q.device)
+    if Kout is None:
+        Kout = torch.empty((N, Hk, D), dtype=t, device=Q.device)
+    if R and (pos is None or pos.shape != (N,)):
+        raise ValueError(f"pos must be [{N}] positions")
+    _check("ssn_qk_norm_rope", lib().ssn_qk_norm_rope(
+        _code(t), N, Hq, Hk, D, R, P, code, e, *_rows(Q, "Q", Q, g, t, (N, Hq, D)),
+        *_rows(K, "K", Q, g, t, (N, Hk, D)), _weight(wq, "wq", Q, g, t, D), _weight(wk, "wk", Q, g, t, D),
+        _gpu(pos, "pos", Q, g, torch.int32, 1) if R else None,
+        _gpu(table, "table", Q, g, torch.float32, 2) if R else None,
+        *_rows(Qout, "Qout", Q, g, t, (N, Hq, D)), *_rows(Kout, "Kout", Q, g, t, (N, Hk, D)),
+        _stream(stream)))
+    return Qout, Kout
+
+
+def qk_norm_rope_workspace(N: int, Hq: int, Hk: int, D: int, device,
+                           dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """A workspace for qk_norm_rope_backward at this shape; calls that share
+    it must not overlap."""
+    n = int(lib().ssn_qk_norm_rope_workspace_bytes(_dt_code(dtype), N, Hq, Hk, D))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def qk_norm_rope_backward(Q: torch.Tensor, K: torch.Tensor, GQ: torch.Tensor, GK: torch.Tensor,
+                          pos: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
+                          wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
+                          eps: Optional[float] = 1e-6, style: str = "halves",
+                          GQin: Optional[torch.Tensor] = None, GKin: Optional[torch.Tensor] = None,
+                          Gwq: Optional[torch.Tensor] = None, Gwk: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of qk_norm_rope for GQ = dL/dQout, GK = dL/dKout.  Returns
+    (dL/dQ, dL/dK, dL/dwq, dL/dwk): the weights' in float32 [D], None where
+    that weight is None."""
+    N, Hq, D = Q.shape
+    Hk = K.shape[1]
+    P, R, code, e = _rotation(table, style, eps, D, wq, wk)
+    t, g, dev = Q.dtype, Q.get_device(), Q.device
+    if GQin is None:
+        GQin = torch.empty((N, Hq, D), dtype=t, device=dev)
+    if GKin is None:
+        GKin = torch.empty((N, Hk, D), dtype=t, device=dev)
+    if wq is None:
+        Gwq = None
+    elif Gwq is None:
+        Gwq = torch.empty(D, dtype=torch.float32, device=dev)
+    if wk is None:
+        Gwk = None
+    elif Gwk is None:
+        Gwk = torch.empty(D, dtype=torch.float32, device=dev)
+    if workspace is None and (Gwq is not None or Gwk is not None):
+        workspace = qk_norm_rope_workspace(N, Hq, Hk, D, dev, t)
+    if R and (pos is None or pos.shape != (N,)):
+        raise ValueError(f"pos must be [{N}] positions")
+    _check("ssn_qk_norm_rope_backward", lib().ssn_qk_norm_rope_backward(
+        _code(t), N, Hq, Hk, D, R, P, code, e, *_rows(Q, "Q", Q, g, t, (N, Hq, D)),
+        *_rows(K, "K", Q, g, t, (N, Hk, D)), _weight(wq, "wq", Q, g, t, D), _weight(wk, "wk", Q, g, t, D),
+        _gpu(pos, "pos", Q, g, torch.int32, 1) if R else None,
+        _gpu(table, "table", Q, g, torch.float32, 2) if R else None,
+        *_rows(GQ, "GQ", Q, g, t, (N, Hq, D)), *_rows(GK, "GK", Q, g, t, (N, Hk, D)),
+        *_rows(GQin, "GQin", Q, g, t, (N, Hq, D)), *_rows(GKin, "GKin", Q, g, t, (N, Hk, D)),
+        _weight(Gwq, "Gwq", Q, g, torch.float32, D), _weight(Gwk, "Gwk", Q, g, torch.float32, D),
+        None if workspace is None else _gpu(workspace, "workspace", Q, g, torch.uint8, 1),
+        0 if workspace is None else workspace.numel(), _stream(stream)))
+    return GQin, GKin, Gwq, Gwk
+
+
+def _paged(Kc, Vc, pages, starts, lens, first, g, t, Hk, D):
+    """(B, C arguments) of a batch of sequences over the paged cache."""
+    if Kc.dim() != 4 or Kc.shape[1] != Hk or Kc.shape[3] != D or Vc.shape != Kc.shape:
+        raise ValueError(f"shape mismatch Kc{tuple(Kc.shape)} Vc{tuple(Vc.shape)}, expected "
+                         f"(pages, {Hk}, page_size, {D})")
+    if pages.dim() != 2:
+        raise ValueError(f"pages must be [B, width], got {tuple(pages.shape)}")
+    B, width = pages.shape
+    if starts.shape != (B + 1,) or lens.shape != (B,):
+        raise ValueError(f"shape mismatch pages{tuple(pages.shape)} starts{tuple(starts.shape)} "
+                         f"lens{tuple(lens.shape)}")
+    return B, (_gpu(Kc, "Kc", first, g, t, 4), _gpu(Vc, "Vc", first, g, t, 4), Kc.shape[0], Kc.shape[2],
+               _gpu(pages, "pages", first, g, torch.int32, 2), width,
+               _gpu(starts, "starts", first, g, torch.int32, 1), _gpu(lens, "lens", first, g, torch.int32, 1))
+
+
+def kv_append(K: torch.Tensor, V: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor,
+              pages: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor,
+              Q: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
+              wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
+              eps: Optional[float] = 1e-6, style: str = "halves",
+              Qout: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Keys [N, Hk, D], normed and rotated to their positions, and values go to
+    their slots of the paged cache, in place; queries (if given) are normed and
+    rotated.  pages [B, width], starts [B + 1] and lens [B] (new tokens
+    included) are int32 device tensors.  Returns Qout (None without Q)."""
+    N, Hk, D = K.shape
+    P, R, code, e = _rotation(table, style, eps, D, wq, wk)
+    t, g = K.dtype, K.get_device()
+    Hq, q, qo = 0, (None, 0), (None, 0)
+    if Q is not None:
+        Hq = Q.shape[1]
+        if Qout is None:
+            Qout = torch.empty((N, Hq, D), dtype=t, device=K.device)
+        q = _rows(Q, "Q", K, g, t, (N, Hq, D))
+        qo = _rows(Qout, "Qout", K, g, t, (N, Hq, D))
+    B, paged = _paged(Kc, Vc, pages, starts, lens, K, g, t, Hk, D)
+    _check("ssn_kv_append", lib().ssn_kv_append(
+        _code(t), N, B, Hq, Hk, D, R, P, code, e, *q, *_rows(K, "K", K, g, t, (N, Hk, D)),
+        *_rows(V, "V", K, g, t, (N, Hk, D)), _weight(wq, "wq", K, g, t, D) if Hq else None,
+        _weight(wk, "wk", K, g, t, D), _gpu(table, "table", K, g, torch.float32, 2) if R else None,
+        *paged, *qo, _stream(stream)))
+    return Qout if Q is not None else None
+
+
+def paged_attention_workspace_bytes(N: int, B: int, Hq: int, Hk: int, D: int, max_q: int, max_len: int,
+                                    dtype: torch.dtype = torch.bfloat16) -> int:
+    return int(lib().ssn_paged_attention_workspace_bytes(_dt_code(dtype), N, B, Hq, Hk, D, max_q, max_len))
+
+
+def paged_attention_workspace(N: int, B: int, Hq: int, Hk: int, D: int, max_q: int, max_len: int, device,
+                              dtype: torch.dtype = torch.bfloat16) -> Optional[torch.Tensor]:
+    """A workspace for paged_attention at this shape (None when it takes no
+    split); calls that share it must not overlap."""
+    n = paged_attention_workspace_bytes(N, B, Hq, Hk, D, max_q, max_len, dtype)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n > 0 else None
+
+
+def paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, pages: torch.Tensor,
+                    starts: torch.Tensor, lens: torch.Tensor, max_q: int, max_len: int,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Attention of new tokens Q [N, Hq, D] over the paged cache that holds
+    their keys and values already: each sees its sequence up to itself.  max_q
+    and max_len bound the new tokens and the length of a sequence (host
+    numbers); scale defaults to D^-1/2; lse [N, Hq] float32 receives the
+    logarithms of the softmax sums.  Without a workspace (1-D uint8, from
+    paged_attention_workspace()) the keys are not split."""
+    N, Hq, D = Q.shape
+    Hk = Kc.shape[1] if Kc.dim() == 4 else 0
+    t, g = Q.dtype, Q.get_device()
+    if out is None:
+        out = torch.empty((N, Hq, D), dtype=t, device=Q.device)
+    if lse is not None and lse.shape != (N, Hq):
+        raise ValueError(f"lse has shape {tuple(lse.shape)}, expected ({N}, {Hq})")
+    B, paged = _paged(Kc, Vc, pages, starts, lens, Q, g, t, Hk, D)
+    _check("ssn_paged_attention", lib().ssn_paged_attention(
+        _code(t), N, B, Hq, Hk, D, max_q, max_len, D ** -0.5 if scale is None else float(scale),
+        *_rows(Q, "Q", Q, g, t, (N, Hq, D)), *paged, *_rows(out, "out", Q, g, t, (N, Hq, D)),
+        None if lse is None else _gpu(lse, "lse", Q, g, torch.float32, 2),
+        None if workspace is None else _gpu(workspace, "workspace", Q, g, torch.uint8, 1),
+        0 if workspace is None else workspace.numel(), _stream(stream)))
+    return out

@@ -1,0 +1,477 @@
+"""The attention sublayer's kernels on the GPU against the float64 oracle:
+norms of heads with the rotation and their gradients, appends to a paged cache,
+attention over it, at the sizes, masks and layouts where they can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+from attn_helpers import (DEV, TORCH, Batch, attention_bound, check_close, dev, packed_rows, poison)
+from helpers import elementwise_bound, rel
+from oracle import attn_oracle as A
+from oracle.ssn_oracle import f64
+from paper_2607_13332_amd import inputs as I
+from paper_2607_13332_amd import ssn
+
+pytestmark = pytest.mark.gpu
+
+# (query heads, key heads, head size, rotated part)
+HEADS = [(40, 8, 128, 128), (16, 16, 64, 64), (3, 1, 256, 256), (4, 2, 128, 64), (5, 5, 80, 80),
+         (2, 1, 33, 32), (1, 1, 1, 0), (2, 2, 1024, 1024), (6, 2, 64, 0), (3, 2, 96, 24)]
+
+
+def _normal(r, shape, dtype, scale=1.0):
+    return I.store(scale * r.standard_normal(shape), dtype)
+
+
+def _case(dtype, heads, N, seed, S=50):
+    Hq, Hk, D, R = heads
+    r = np.random.default_rng(seed)
+    q, k = _normal(r, (N, Hq, D), dtype, 2.0), _normal(r, (N, Hk, D), dtype, 0.5)
+    wq, wk = (I.store(1 + 0.2 * r.standard_normal(D), dtype) for _ in range(2))
+    pos = r.integers(0, S, N).astype(np.int32)
+    table = A.rope_table(S, R, 5e5).astype(np.float32) if R else None
+    return r, q, k, wq, wk, pos, table
+
+
+def _on_gpu(pos, table):
+    return (None, None) if table is None else (torch.from_numpy(pos).to(DEV), torch.from_numpy(table).to(DEV))
+
+
+def _norm_bound(x, w, pos, table, eps, style, ref, dtype):
+    """The float32 steps: D/2 terms at most in a chain of the sum of squares
+    (half of its error reaches the root), then a handful of roundings."""
+    D = x.shape[-1]
+    ab = None if table is None else np.abs(table)
+    # |n1 cos| + |n2 sin|: the rotation of absolute values, signs dropped
+    R = 0 if table is None else table.shape[1]
+    n = np.abs(A.norm_rope(x, w, eps=eps))
+    mag = n.copy()
+    if R:
+        c, s = ab[pos][:, None, :R // 2], ab[pos][:, None, R // 2:]
+        f, g = (slice(0, R // 2), slice(R // 2, R)) if style == "halves" else (slice(0, R, 2), slice(1, R, 2))
+        mag[..., f], mag[..., g] = n[..., f] * c + n[..., g] * s, n[..., f] * s + n[..., g] * c
+    return elementwise_bound(ref, mag, D // 4 + 8, False, dtype == "bf16")
+
+
+@pytest.mark.parametrize("P,R,theta", [(1, 2, 1e4), (70, 128, 5e5), (131072, 64, 1e4), (5, 0, 3.0)])
+def test_rope_table(P, R, theta):
+    got = ssn.rope_table(P, R, theta, device=DEV).cpu().numpy()
+    ref = A.rope_table(P, R, theta)
+    # float64 sines of float64 angles: an angle a is off by a few 2^-53 a
+    assert np.abs(got - ref).max(initial=0) <= 2.0 ** -24 + 8 * P * 2.0 ** -53
+
+
+@pytest.mark.parametrize("style", ["halves", "pairs"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", HEADS)
+def test_norm_rope(dtype, heads, style):
+    for N, eps, weights in [(1, 1e-6, True), (37, 0.1, True), (130, 1e-6, False), (9, None, False)]:
+        r, q, k, wq, wk, pos, table = _case(dtype, heads, N, N)
+        if not weights:
+            wq = wk = None
+        print(f"[case] norm_rope {dtype} {heads} {style} N={N} eps={eps}", flush=True)
+        w = [None if a is None else dev(a, dtype) for a in (wq, wk)]
+        p, t = _on_gpu(pos, table)
+        Q, K = ssn.qk_norm_rope(dev(q, dtype), dev(k, dtype), p, t, *w, eps=eps, style=style)
+        for got, x, ww in ((Q, q, wq), (K, k, wk)):
+            ref = A.norm_rope(x, ww, pos, table, eps, style)
+            check_close("norm_rope", I.to_host(got), ref, _norm_bound(x, ww, pos, table, eps, style, ref, dtype))
+
+
+@pytest.mark.parametrize("style", ["halves", "pairs"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", HEADS)
+def test_norm_rope_backward(dtype, heads, style):
+    Hq, Hk, D, R = heads
+    for N, eps, weights in [(1, 1e-6, True), (150, 0.1, True), (33, 1e-6, False), (9, None, False)]:
+        r, q, k, wq, wk, pos, table = _case(dtype, heads, N, 100 + N)
+        if not weights:
+            wq = wk = None
+        gq, gk = _normal(r, q.shape, dtype), _normal(r, k.shape, dtype)
+        print(f"[case] norm_rope backward {dtype} {heads} {style} N={N} eps={eps}", flush=True)
+        w = [None if a is None else dev(a, dtype) for a in (wq, wk)]
+        p, t = _on_gpu(pos, table)
+        args = (dev(q, dtype), dev(k, dtype), dev(gq, dtype), dev(gk, dtype), p, t)
+        GQ, GK, Gwq, Gwk = ssn.qk_norm_rope_backward(*args, *w, eps=eps, style=style)
+        again = ssn.qk_norm_rope_backward(*args, *w, eps=eps, style=style)
+        for x, y in zip((GQ, GK, Gwq, Gwk), again):
+            assert x is y is None or torch.equal(x, y)
+        for got, gw, x, gy, ww in ((GQ, Gwq, q, gq, wq), (GK, Gwk, k, gk, wk)):
+            ref, ref_w = A.norm_rope_backward(x, gy, ww, pos, table, eps, style)
+            f, g = f64(x), f64(gy)
+            rr = 1.0 if eps is None else 1 / np.sqrt((f * f).mean(-1, keepdims=True) + eps)
+            # |rotated gy| <= |a| + |b| of its pair: bounded by the pair's sum
+            turned = np.abs(A.norm_rope_backward(np.ones_like(f), g, None, pos, table, None, style)[0])
+            turned = np.maximum(turned, np.abs(g).max(-1, keepdims=True))
+            h = turned * (1.0 if ww is None else np.abs(f64(ww)))
+            n = np.abs(f) * rr
+            mag = h if eps is None else rr * (h + n * (h * n).mean(-1, keepdims=True))
+            check_close("dL/dx", I.to_host(got), ref, elementwise_bound(ref, mag, D // 2 + 12, False, dtype == "bf16"))
+            if ww is None:
+                assert gw is None
+            else:
+                check_close("dL/dw", I.to_host(gw), ref_w,
+                            elementwise_bound(ref_w, (turned * n).sum((0, 1)), 256, False, False))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_norm_rope_strided(dtype, odd):
+    """Parts of packed rows; `odd` moves them off the 16-byte grid."""
+    heads = (8, 2, 128, 128)
+    r, q, k, wq, wk, pos, table = _case(dtype, heads, 41, 3)
+    gq, gk = _normal(r, q.shape, dtype), _normal(r, k.shape, dtype)
+    p, t = _on_gpu(pos, table)
+    w = (dev(wq, dtype), dev(wk, dtype))
+    plain = ssn.qk_norm_rope(dev(q, dtype), dev(k, dtype), p, t, *w)
+    plain_b = ssn.qk_norm_rope_backward(dev(q, dtype), dev(k, dtype), dev(gq, dtype), dev(gk, dtype), p, t, *w)
+    both = packed_rows(np.concatenate([q, k], 1), dtype, ld_extra=64 + odd, before=odd)
+    outs = [packed_rows(np.zeros((41, 10, 128)).astype(q.dtype), dtype, ld_extra=128 + odd, before=64)
+            for _ in range(2)]
+    grad = packed_rows(np.concatenate([gq, gk], 1), dtype, ld_extra=odd)
+    Q, K = ssn.qk_norm_rope(both[:, :8], both[:, 8:], p, t, *w, Qout=outs[0][:, :8], Kout=outs[0][:, 8:])
+    G = ssn.qk_norm_rope_backward(both[:, :8], both[:, 8:], grad[:, :8], grad[:, 8:], p, t, *w,
+                                  GQin=outs[1][:, :8], GKin=outs[1][:, 8:])
+    # the generic kernel sums in another order: float32 roundings apart
+    for got, ref in zip((Q, K, *G), (*plain, *plain_b)):
+        assert rel(I.to_host(got), f64(I.to_host(ref))) <= (1e-3 if dtype == "bf16" and got.dim() > 1 else 1e-6)
+    for o in outs:
+        base = o._base if o._base is not None else o
+        assert (base[:, :64] == 7).all() and (base[:, 64 + 1280:] == 7).all()
+
+
+def test_norm_rope_empty_and_extreme_rows():
+    w = torch.ones(128, dtype=torch.bfloat16, device=DEV)
+    none = torch.empty((0, 4, 128), dtype=torch.bfloat16, device=DEV)
+    table = ssn.rope_table(4, 128, device=DEV)
+    pos = torch.empty(0, dtype=torch.int32, device=DEV)
+    Q, K = ssn.qk_norm_rope(none, none, pos, table, w, w)
+    assert Q.shape == K.shape == (0, 4, 128)
+    out = ssn.qk_norm_rope_backward(none, none, none, none, pos, table, w, w)
+    assert (out[2] == 0).all() and (out[3] == 0).all()
+    # a zero head stays zero (eps keeps the root off zero); a NaN stays in its head
+    x = torch.randn((3, 4, 128), device=DEV).bfloat16()
+    x[0, 1] = 0
+    x[2, 3, 5] = float("nan")
+    pos = torch.tensor([0, 1, 2], dtype=torch.int32, device=DEV)
+    Q, K = ssn.qk_norm_rope(x, x, pos, table, w, w)
+    assert (Q[0, 1] == 0).all() and torch.isnan(Q[2, 3]).all()
+    bad = torch.isnan(Q)
+    bad[2, 3] = False
+    assert not bad.any() and torch.equal(Q.nan_to_num(1e3), K.nan_to_num(1e3))
+
+
+BATCHES = {
+    "one": [(1, 1)],
+    "tokens": [(1, 5), (1, 64), (0, 0), (1, 65), (1, 1000), (0, 9), (1, 128)],
+    "chunks": [(3, 3), (17, 40), (0, 7), (130, 130), (5, 700)],
+    "mixed": [(1, 300), (200, 333), (1, 1), (1, 77), (64, 64)],
+    "empty rows": [(2, 1), (1, 0), (5, 2), (1, 3)],
+    "long": [(70, 2500), (1, 3001)],
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", HEADS)
+def test_kv_append(dtype, heads):
+    Hq, Hk, D, R = heads
+    for name, page, style in [("tokens", 16, "halves"), ("chunks", 64, "pairs"), ("empty rows", 3, "halves"),
+                              ("mixed", 1, "pairs")]:
+        bt = Batch(BATCHES[name], Hk, D, page, dtype, 5, first=2, pad=3)
+        r, q, k, wq, wk, _, table = _case(dtype, heads, bt.N, 7, S=1100)
+        v = _normal(r, (bt.N, Hk, D), dtype)
+        v[2] = poison(dtype)[0]                    # values are moved as they are
+        print(f"[case] kv_append {dtype} {heads} {name} page={page}", flush=True)
+        Kc, Vc, pages, starts, lens = bt.device()
+        Qout = torch.full((bt.N, Hq, D), 7.0, dtype=TORCH[dtype], device=DEV)
+        t = None if table is None else torch.from_numpy(table).to(DEV)
+        ssn.kv_append(dev(k, dtype), dev(v, dtype), Kc, Vc, pages, starts, lens, Q=dev(q, dtype), table=t,
+                      wq=dev(wq, dtype), wk=dev(wk, dtype), style=style, Qout=Qout)
+        rows = [(i, b, p) for i, b, p in A.batch_rows(bt.starts, bt.lens) if p >= 0]
+        at = np.array([i for i, _, _ in rows])
+        pos = np.array([p for _, _, p in rows])
+        refk = A.norm_rope(k[at], wk, pos, table, 1e-6, style)
+        refq = A.norm_rope(q[at], wq, pos, table, 1e-6, style)
+        got_q, got_k, got_v = I.to_host(Qout), I.to_host(Kc), I.to_host(Vc)
+        slots = np.array([bt.pages[b, p // page] for _, b, p in rows]), pos % page
+        check_close("Qout", got_q[at], refq, _norm_bound(q[at], wq, pos, table, 1e-6, style, refq, dtype))
+        check_close("Kc", got_k[slots[0], :, slots[1]], refk,
+                    _norm_bound(k[at], wk, pos, table, 1e-6, style, refk, dtype))
+        # the values bit for bit, and nothing else of the caches or of Qout touched
+        bits = lambda a: np.ascontiguousarray(a).view(np.uint16 if dtype == "bf16" else np.uint32)  # noqa: E731
+        want_k, want_v = bt.Kc.copy(), bt.Vc.copy()
+        want_v[slots[0], :, slots[1]] = v[at]
+        want_k[slots[0], :, slots[1]] = got_k[slots[0], :, slots[1]]
+        assert np.array_equal(bits(got_v), bits(want_v)) and np.array_equal(bits(got_k), bits(want_k))
+        rest = np.setdiff1d(np.arange(bt.N), at)
+        assert (f64(got_q[rest]) == 7).all()
+        # without queries: the same caches
+        Kc2, Vc2, *_ = bt.device()
+        assert ssn.kv_append(dev(k, dtype), dev(v, dtype), Kc2, Vc2, pages, starts, lens, table=t,
+                             wk=dev(wk, dtype), style=style) is None
+        assert np.array_equal(bits(I.to_host(Kc2)), bits(want_k))
+        assert np.array_equal(bits(I.to_host(Vc2)), bits(want_v))
+
+
+ATTN_HEADS = [(40, 8, 128), (16, 16, 64), (14, 2, 64), (7, 1, 128), (3, 1, 256), (6, 2, 80), (2, 1, 33), (4, 4, 8),
+              (2, 1, 300), (32, 1, 128)]
+
+
+def _attend(bt, Hq, Hk, D, dtype, seed, split=True, q=None, with_lse=True, scale=None, strided=False):
+    r = np.random.default_rng(seed)
+    if q is None:
+        q = _normal(r, (bt.N, Hq, D), dtype, 1.5)
+    Kc, Vc, pages, starts, lens = bt.device()
+    ws = ssn.paged_attention_workspace(bt.N, len(bt.lens), Hq, Hk, D, bt.max_q, bt.max_len, DEV,
+                                       dtype=TORCH[dtype]) if split else None
+    if ws is not None:
+        ws.fill_(255)                              # NaN in any type
+    Q = packed_rows(q, dtype, ld_extra=2 * Hk * D) if strided else dev(q, dtype)
+    out = torch.full((bt.N, Hq, D), 7.0, dtype=TORCH[dtype], device=DEV)
+    lse = torch.full((bt.N, Hq), 7.0, dtype=torch.float32, device=DEV) if with_lse else None
+    ssn.paged_attention(Q, Kc, Vc, pages, starts, lens, bt.max_q, bt.max_len, scale=scale, out=out, lse=lse,
+                        workspace=ws)
+    return q, I.to_host(out), None if lse is None else lse.cpu().numpy()
+
+
+def _check_attention(bt, Hq, Hk, D, dtype, q, out, lse, scale=None):
+    scale = D ** -0.5 if scale is None else scale
+    O, L, M = A.paged_attention(q, bt.Kc, bt.Vc, bt.pages, bt.starts, bt.lens, scale)
+    kmax = max([np.abs(A.gather(bt.Kc, bt.pages[b], t)).max(initial=0) for b, t in enumerate(bt.lens)])
+    inside = ~np.isnan(L[:, 0])
+    assert (f64(out[~inside]) == 7).all()
+    bound = attention_bound(O, M, q, kmax, D, scale, bt.max_len, dtype)
+    check_close("O", out[inside], O[inside], bound[inside])
+    # scores of ordinary size: a flat bar as well (a float32 score of 200 alone is off by 1e-5)
+    if inside.any() and scale == D ** -0.5 and np.abs(O[inside]).max(initial=0) > 0:
+        assert rel(out[inside], O[inside]) <= (3e-3 if dtype == "bf16" else 3e-6)
+    if lse is not None:
+        assert (lse[~inside] == 7).all()
+        reach = abs(scale) * np.abs(f64(q)).sum(-1) * kmax
+        check_close("lse", lse[inside], L[inside],
+                    (2.0 ** -20 + (D + 8) * 2.0 ** -22 * reach + bt.max_len * 2.0 ** -23)[inside])
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", ATTN_HEADS)
+def test_paged_attention(dtype, heads, split):
+    Hq, Hk, D = heads
+    for n, (name, page) in enumerate([("one", 16), ("tokens", 16), ("chunks", 64), ("mixed", 7), ("empty rows", 1),
+                                      ("long", 100), ("mixed", 128)]):
+        if Hq * D > 2000 and name == "long" and not split:
+            continue
+        bt = Batch(BATCHES[name], Hk, D, page, dtype, 11 + n, first=n % 3, pad=n % 2)
+        print(f"[case] paged_attention {dtype} {heads} {name} page={page} split={split}", flush=True)
+        q, out, lse = _attend(bt, Hq, Hk, D, dtype, n, split, with_lse=n % 2 == 0, strided=n % 3 == 1)
+        _check_attention(bt, Hq, Hk, D, dtype, q, out, lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("seqs", [[(1, 4000)], [(1, 9000), (1, 50)], [(300, 700)], [(20, 3000), (40, 41)]])
+def test_repeated_calls_give_the_same_bits(dtype, seqs):
+    bt = Batch(seqs, 2, 128, 64, dtype, 3)
+    q, one, lse1 = _attend(bt, 10, 2, 128, dtype, 1)
+    _, two, lse2 = _attend(bt, 10, 2, 128, dtype, 1, q=q)
+    assert np.array_equal(one, two) and np.array_equal(lse1, lse2)
+    _check_attention(bt, 10, 2, 128, dtype, q, one, lse1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,length,Hq", [(1, 600, 4), (9, 9, 4), (200, 200, 4), (140, 1500, 2), (3, 400, 10)])
+def test_what_a_row_does_not_see_has_no_effect(dtype, D, new, length, Hq):
+    """Infinities and NaN in keys and values of later positions: rows before
+    them keep their bits."""
+    bt = Batch([(new, length)], 2, D, 16, dtype, 5)
+    q, clean, _ = _attend(bt, Hq, 2, D, dtype, 2)
+    _check_attention(bt, Hq, 2, D, dtype, q, clean, None)
+    for at in {new - 1, new // 2, min(1, new - 1)}:
+        bad = Batch([(new, length)], 2, D, 16, dtype, 5)
+        page, off = bad.slots(0)
+        for j in range(length - new + at, length):
+            bad.Vc[page[j], :, off[j]] = poison(dtype)[j % 3]
+            if j % 2:
+                bad.Kc[page[j], :, off[j]] = poison(dtype)[(j + 1) % 3]
+        _, out, _ = _attend(bad, Hq, 2, D, dtype, 2, q=q)
+        assert np.array_equal(out[:at], clean[:at]), at
+        # a row that sees a NaN, or an infinite value with a weight, is not finite
+        assert not np.isfinite(f64(out[at:])).any() or new == 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinite_values_that_a_row_sees(dtype):
+    """An infinite value in one element reaches that element of the rows that
+    see it, with its sign, and no other."""
+    new, length = 70, 200
+    bt = Batch([(new, length)], 1, 64, 16, dtype, 5)
+    q, clean, _ = _attend(bt, 2, 1, 64, dtype, 2)
+    page, off = bt.slots(0)
+    j = length - 30
+    bt.Vc[page[j], 0, off[j], 7] = poison(dtype)[1]
+    bt.Vc[page[j], 0, off[j], 9] = poison(dtype)[2]
+    _, out, _ = _attend(bt, 2, 1, 64, dtype, 2, q=q)
+    got, want = f64(out), f64(clean)
+    first = new - 30
+    assert (got[first:, :, 7] == np.inf).all() and (got[first:, :, 9] == -np.inf).all()
+    keep = np.ones(64, bool)
+    keep[[7, 9]] = False
+    assert np.array_equal(got[..., keep], want[..., keep]) and np.array_equal(got[:first], want[:first])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 4.0])
+def test_scales_and_far_scores(dtype, scale):
+    """Scores far apart (scale 4: hundreds), equal ones, a negative scale."""
+    bt = Batch([(40, 300), (1, 2000)], 2, 128, 16, dtype, 8)
+    q, out, lse = _attend(bt, 4, 2, 128, dtype, 1, scale=scale)
+    _check_attention(bt, 4, 2, 128, dtype, q, out, lse, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_sequence_of_growing_scores(dtype):
+    """Every key scores higher than all before it: the running maximum moves
+    at every tile."""
+    bt = Batch([(65, 1000), (1, 1000)], 1, 64, 16, dtype, 8)
+    for b in range(2):
+        page, off = bt.slots(b)
+        ramp = np.zeros((1000, 1, 64))
+        ramp[:, 0, 0] = np.linspace(0, 30, 1000)
+        bt.Kc[page, :, off] = I.store(ramp, dtype)
+    q = np.zeros((bt.N, 2, 64))
+    q[:, :, 0] = 16.0
+    q = I.store(q, dtype)
+    _, out, lse = _attend(bt, 2, 1, 64, dtype, 1, q=q)
+    _check_attention(bt, 2, 1, 64, dtype, q, out, lse)
+
+
+def test_other_stream_and_no_sync():
+    """On a side stream, ordered after the work that makes the inputs there."""
+    bt = Batch([(1, 500), (60, 900)], 2, 128, 64, "bf16", 5)
+    q, ref, _ = _attend(bt, 8, 2, 128, "bf16", 2)
+    Kc, Vc, pages, starts, lens = bt.device()
+    ws = ssn.paged_attention_workspace(bt.N, 2, 8, 2, 128, bt.max_q, bt.max_len, DEV)
+    Q = dev(q, "bf16")
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        K2, V2 = torch.zeros_like(Kc), torch.zeros_like(Vc)
+        out = torch.empty_like(Q)
+        torch.cuda._sleep(2_000_000)
+        K2.copy_(Kc)
+        V2.copy_(Vc)
+        ssn.paged_attention(Q, K2, V2, pages, starts, lens, bt.max_q, bt.max_len, out=out, workspace=ws)
+    st.synchronize()
+    assert np.array_equal(I.to_host(out), ref)
+
+
+def test_graph_of_a_decode_step_follows_its_lengths():
+    """One captured step (append, attention) replayed while the sequences
+    grow, eager work between the replays, each replay against the eager call."""
+    Hq, Hk, D, page, T = 8, 2, 128, 16, 90
+    r = np.random.default_rng(3)
+    bt = Batch([(1, 70), (1, 3), (1, 31)], Hk, D, page, "bf16", 5, extra_width=4, extra_pages=20)
+    used = set(int(p) for b in range(3) for p in bt.slots(b)[0])
+    free = [p for p in range(bt.Kc.shape[0]) if p not in used]
+    for b in range(3):
+        have = -(-int(bt.lens[b]) // page)
+        for j in range(have, bt.pages.shape[1]):
+            if free:
+                bt.pages[b, j] = free.pop()
+    Kc, Vc, pages, starts, lens = bt.device()
+    table = ssn.rope_table(T + 100, D, 5e5, device=DEV)
+    w = torch.ones(D, dtype=torch.bfloat16, device=DEV)
+    qkv = torch.zeros((3, (Hq + 2 * Hk) * D), dtype=torch.bfloat16, device=DEV)
+    heads = qkv.view(3, Hq + 2 * Hk, D)
+    Qr, O = (torch.zeros((3, Hq, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ws = ssn.paged_attention_workspace(3, 3, Hq, Hk, D, 1, T, DEV)
+
+    def step(Qr, O, Kc, Vc):
+        ssn.kv_append(heads[:, Hq:Hq + Hk], heads[:, Hq + Hk:], Kc, Vc, pages, starts, lens, Q=heads[:, :Hq],
+                      table=table, wq=w, wk=w, Qout=Qr)
+        ssn.paged_attention(Qr, Kc, Vc, pages, starts, lens, 1, T, out=O, workspace=ws)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        step(Qr, O, Kc, Vc)
+    torch.cuda.current_stream().wait_stream(st)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(Qr, O, Kc, Vc)
+    for n in range(6):
+        qkv.copy_(dev(_normal(r, tuple(qkv.shape), "bf16"), "bf16"))
+        lens += 1
+        K2, V2, Q2, O2 = Kc.clone(), Vc.clone(), torch.zeros_like(Qr), torch.zeros_like(O)
+        g.replay()
+        step(Q2, O2, K2, V2)
+        torch.cuda.synchronize()
+        assert torch.equal(O, O2) and torch.equal(Kc.view(torch.int16), K2.view(torch.int16)), n
+        assert torch.isfinite(O.float()).all() and (O != 0).any()
+    assert int(lens[0]) == 76
+
+
+def test_cache_past_two_gibi_elements():
+    """A cache of more than 2^31 elements, its last pages in use."""
+    Hk, D, page = 8, 128, 64
+    npages = 2 ** 31 // (Hk * D * page) + 40
+    Kc = torch.zeros((npages, Hk, page, D), dtype=torch.bfloat16, device=DEV)
+    Vc = torch.zeros_like(Kc)
+    bt = Batch([(1, 200), (130, 150)], Hk, D, page, "bf16", 3, extra_pages=1)
+    last = npages - bt.Kc.shape[0]
+    Kc[last:], Vc[last:] = dev(bt.Kc, "bf16"), dev(bt.Vc, "bf16")
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)  # noqa: E731
+    pages = np.where((bt.pages >= 0) & (bt.pages < bt.Kc.shape[0]), bt.pages + last, bt.pages).astype(np.int32)
+    r = np.random.default_rng(0)
+    q = _normal(r, (bt.N, 16, D), "bf16", 1.5)
+    ws = ssn.paged_attention_workspace(bt.N, 2, 16, Hk, D, bt.max_q, bt.max_len, DEV)
+    out = ssn.paged_attention(dev(q, "bf16"), Kc, Vc, i32(pages), i32(bt.starts), i32(bt.lens), bt.max_q, bt.max_len,
+                              workspace=ws)
+    _check_attention(bt, 16, Hk, D, "bf16", q, I.to_host(out), None)
+    k = _normal(r, (bt.N, Hk, D), "bf16")
+    ssn.kv_append(dev(k, "bf16"), dev(k, "bf16"), Kc, Vc, i32(pages), i32(bt.starts), i32(bt.lens), eps=None)
+    for i, b, p in A.batch_rows(bt.starts, bt.lens):
+        got = I.to_host(Kc[int(pages[b, p // page]), :, p % page])
+        assert np.array_equal(got, k[i])
+
+
+def test_wrappers_refuse():
+    bt = Batch([(1, 20), (3, 9)], 2, 64, 16, "bf16", 3)
+    Kc, Vc, pages, starts, lens = bt.device()
+    Q = torch.zeros((4, 4, 64), dtype=torch.bfloat16, device=DEV)
+    K = torch.zeros((4, 2, 64), dtype=torch.bfloat16, device=DEV)
+    att = lambda *a, **k: ssn.paged_attention(*a, 3, 20, **k)  # noqa: E731
+    with pytest.raises(TypeError, match="Kc must be torch.bfloat16"):
+        att(Q, Kc.float(), Vc, pages, starts, lens)
+    with pytest.raises(ValueError, match="Kc must be contiguous"):
+        att(Q, Kc.transpose(2, 3).contiguous().transpose(2, 3), Vc, pages, starts, lens)
+    with pytest.raises(ValueError, match="shape mismatch"):
+        att(Q, Kc, Vc[:-1], pages, starts, lens)
+    with pytest.raises(ValueError, match="shape mismatch"):
+        att(Q, Kc, Vc, pages, starts[:-1], lens)
+    with pytest.raises(TypeError, match="pages must be torch.int32"):
+        att(Q, Kc, Vc, pages.long(), starts, lens)
+    with pytest.raises(ValueError, match="heads of a row"):
+        att(Q.transpose(0, 1).contiguous().transpose(0, 1), Kc, Vc, pages, starts, lens)
+    with pytest.raises(ValueError, match="out has shape"):
+        att(Q, Kc, Vc, pages, starts, lens, out=Q[:3])
+    with pytest.raises(ValueError, match="different devices"):
+        att(Q, Kc, Vc, pages.cpu(), starts, lens)
+    with pytest.raises(ssn.SSNError, match="status 7"):
+        att(Q, Kc, Vc, pages, starts, lens, out=Q)
+    with pytest.raises(ssn.SSNError, match="status 2"):          # 3 query heads over 2 key heads
+        att(Q[:, :3].contiguous(), Kc, Vc, pages, starts, lens)
+    with pytest.raises(ValueError, match="style"):
+        ssn.kv_append(K, K.clone(), Kc, Vc, pages, starts, lens, style="neox")
+    with pytest.raises(ValueError, match="without a norm"):
+        ssn.qk_norm_rope(Q, K, wq=torch.ones(64, dtype=torch.bfloat16, device=DEV), eps=None)
+    with pytest.raises(ValueError, match="pos must be"):
+        ssn.qk_norm_rope(Q, K, None, ssn.rope_table(4, 64, device=DEV))
+    with pytest.raises(ssn.SSNError, match="status 2"):          # a table wider than the head
+        ssn.qk_norm_rope(Q, K, torch.zeros(4, dtype=torch.int32, device=DEV), ssn.rope_table(4, 128, device=DEV))
+    with pytest.raises(ssn.SSNError, match="status 2"):          # a workspace that is too small
+        w = torch.ones(64, dtype=torch.bfloat16, device=DEV)
+        ssn.qk_norm_rope_backward(Q, K, Q, K, wq=w, wk=w, workspace=torch.zeros(16, dtype=torch.uint8, device=DEV))
+    with pytest.raises(ValueError, match="GPU tensor"):
+        c = torch.zeros((4, 4, 64))
+        ssn.qk_norm_rope(c, c)
