@@ -22,7 +22,8 @@ LIB = os.path.join(PKG, "libssn.so")
 SOURCES = ["ssn_api.hip", "noalloc.hip", "codec_kernels.hip", "decompress_kernels.hip",
            "decompress_f32.hip", "f32_kernels.hip", "f32_weights.hip",
            "f32_strips_a.hip", "f32_strips_b.hip", "weights_kernels.hip", "reparam_kernels.hip",
-           "sparta_kernels.hip", "attn_api.hip", "rope_kernels.hip", "paged_attn.hip"]
+           "sparta_kernels.hip", "attn_api.hip", "rope_kernels.hip", "paged_attn.hip",
+           "attn_tiles_bf16.hip", "attn_tiles_f32.hip", "attn_rows_bf16.hip", "attn_rows_f32.hip"]
 ARCH = "gfx950"
 
 

@@ -12,7 +12,9 @@
 namespace {
 
 constexpr int64_t kMaxElems = (int64_t)1 << 56;   // keeps every byte offset in int64
-constexpr int64_t kMaxRows = (int64_t)1 << 31;    // rows of heads, cache rows, positions
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 4096;   // rows of heads, cache rows, positions
+constexpr int64_t kMaxAttnRows = (int64_t)1 << 29;         // of attention: one grid holds its blocks
+constexpr int64_t kMaxAttnSeqs = (int64_t)1 << 22;         // sequences times key heads, the same
 constexpr int64_t kMaxD = 1024;
 constexpr int64_t kMaxB = 1 << 20;
 
@@ -89,7 +91,7 @@ ssn::PagedBatch paged_batch(int64_t N, int64_t B, int64_t npages, int64_t page_s
   pb.npages = (int32_t)npages;
   pb.B = (int32_t)B;
   pb.N = (int32_t)N;
-  pb.max_len = (int32_t)(max_len < width * page_size ? max_len : width * page_size);
+  pb.max_len = (int32_t)(max_len < width * page_size ? max_len : width * page_size);   // < kMaxRows
   pb.page = ssn::fast_div((uint32_t)page_size);
   return pb;
 }
@@ -222,7 +224,8 @@ ssn_status_t ssn_kv_append(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq, 
 static bool attention_shape_ok(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
                                int64_t max_len) {
   return N >= 0 && B >= 0 && B < kMaxB && Hk >= 1 && Hq >= Hk && Hq <= (1 << 20) && Hq % Hk == 0 && D >= 1 &&
-         max_q >= 0 && max_q < kMaxRows && max_len >= 0 && max_len < kMaxRows && below(N, Hq, kMaxRows);
+         max_q >= 0 && max_q < kMaxRows && max_len >= 0 && max_len < kMaxRows && below(N, Hq, kMaxAttnRows) &&
+         below(B, Hk, kMaxAttnSeqs);
 }
 
 size_t ssn_paged_attention_workspace_bytes(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk,

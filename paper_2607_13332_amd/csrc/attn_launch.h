@@ -71,9 +71,31 @@ struct AttnArgs {
   int max_q;
   float scale;
 };
+// A sequence's rows of one key head are its new tokens times the G heads of
+// the group: row r is token r / G, head r % G.  Sequences of up to `few` rows
+// run the rows kernel, whose waves share the keys; the others the tile kernel,
+// whose waves share the rows.  Each kernel splits the keys into ranges of
+// `chunk`; where a sequence (rows kernel) or row tile (tile kernel) has more
+// than one, partial results are staged and joined: O unnormalized and (m, l)
+// of every row, range by range.
+struct AttnPart {
+  int blocks;           // 16-row blocks of a wave (0: kernel not launched)
+  int chunk, ranges;    // keys of a range, ranges of the longest sequence
+  float* o;             // [range][stage_rows][D]
+  float* ml;            // [range][stage_rows][2]
+  int64_t stage_rows;
+};
+struct AttnPlan {
+  int few;
+  AttnPart rows, tiles;
+};
 // Bytes of workspace that allow every split (0: none).
 size_t attention_workspace_bytes(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D,
                                  int64_t max_q, int64_t max_len);
+hipError_t launch_attn_rows_bf16(const AttnArgs& a, const AttnPlan& p, hipStream_t st);
+hipError_t launch_attn_rows_f32(const AttnArgs& a, const AttnPlan& p, hipStream_t st);
+hipError_t launch_attn_tiles_bf16(const AttnArgs& a, const AttnPlan& p, hipStream_t st);
+hipError_t launch_attn_tiles_f32(const AttnArgs& a, const AttnPlan& p, hipStream_t st);
 hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
 
 }  // namespace ssn

@@ -1,0 +1,224 @@
+// Paged attention of many rows: a block of 4 waves owns a tile of rows of one
+// sequence and key head (64 QB rows, 16 QB to a wave) and walks the keys the
+// tile sees.
+#pragma once
+
+#include "attn_mma.h"
+
+namespace ssn {
+
+typedef __attribute__((address_space(3))) uint32_t lds_word;
+typedef __attribute__((address_space(1))) const uint32_t global_word;
+
+// Tile of rows `tile` of the launch: sequence b has the slots from starts[b] *
+// G / BM + b on, which leaves ceil(rows / BM) to each.
+__device__ __forceinline__ int first_tile(const PagedBatch& pb, int b, int G, int BM) {
+  return (int)((int64_t)clampi(pb.starts[b], 0, pb.N) * G / BM) + b;
+}
+inline int64_t tile_slots(int64_t N, int64_t B, int64_t G, int64_t BM) { return N * G / BM + B; }
+
+// What a wave does with its rows when its keys are done: the result, or its
+// part of it.  Row r of the sequence's rows is token r / G, head r % G.
+template <typename T, int DT, int QB, bool EXACT>
+__device__ __forceinline__ void finish_rows(const AttnArgs& a, const AttnPart& part, RowState<DT / 16, QB>& rs,
+                                            const int (&row)[QB], const int (&seen)[QB], int rows, int s0,
+                                            int kh, int range, int64_t stage0, bool whole, float c, int lane) {
+  const int h4 = 4 * (lane >> 4);
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    const float l = column_sum(rs.l[q]);
+    if (row[q] >= rows) continue;
+    const int token = s0 + row[q] / a.G, head = kh * a.G + row[q] % a.G;
+    const int64_t at = (int64_t)token * a.Hq + head;
+    if (whole) {
+      // 0 / 0 where every score a row sees is -inf; a row that sees nothing is zero
+      const float inv = seen[q] < 0 ? 0.f : 1.f / l;
+      T* out = (T*)a.O + token * a.ldo + (int64_t)head * a.D;
+#pragma unroll
+      for (int d = 0; d < DT / 16; ++d)
+        if (EXACT || 16 * d + h4 < a.D) store4(out + 16 * d + h4, rs.o[d][q] * inv);
+      if (a.lse && lane < 16)
+        a.lse[at] = seen[q] < 0 ? kNegInf : (rs.m[q] * c + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    } else {
+      // (stage0 < 0: rows staged by token and head, else from there in row order)
+      const int64_t to = range * part.stage_rows + (stage0 < 0 ? at : stage0 + row[q]);
+      float* out = part.o + to * a.D;
+#pragma unroll
+      for (int d = 0; d < DT / 16; ++d)
+        if (EXACT || 16 * d + h4 < a.D) *(f32x4*)(out + 16 * d + h4) = rs.o[d][q];
+      if (lane < 16) {
+        float* ml = part.ml + 2 * to;
+        ml[0] = rs.m[q] * c;
+        ml[1] = l;
+      }
+    }
+  }
+}
+
+// Q^T of 16 rows as B operands: lane's row is lane % 16, chunk c of 64 bytes
+// at lane / 16.  `flip`: the sign bits of a negative scale.
+template <int NC, bool EXACT>
+__device__ __forceinline__ void load_query(const char* p, int bytes, int lane, uint32_t flip, bool zero,
+                                           u32x4 (&q)[NC]) {
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int at = c * 64 + (lane >> 4) * 16;
+    u32x4 v = {0, 0, 0, 0};
+    if (!zero && (EXACT || at < bytes)) v = *(const u32x4*)(p + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[c][i] = v[i] ^ flip;
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t sign_bits(float scale) {
+  return scale < 0.f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
+}
+
+template <typename T, int DT, int QB, bool EXACT>
+__global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void paged_attn_tiles(AttnArgs a, AttnPart part, int few, int slots) {
+  using M = Mma<T>;
+  constexpr int RB = DT * (int)sizeof(T), TK = RB <= 256 ? 64 : 32, NKB = TK / 16, NC = RB / 64;
+  constexpr int CH = RB / 16, RPI = kWave / CH, NI = TK / RPI / 4, BM = 64 * QB;
+  __shared__ __align__(1024) char lds[2][2][TK * RB];     // [buffer][K, V]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kh = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
+  // a sequence's last tiles see the most keys: they go first
+  const int slot = slots - 1 - rest % slots, range = rest / slots;
+  const int b = last_at_most(a.pb.B, slot, [&](int i) { return first_tile(a.pb, i, a.G, BM); });
+  const Sequence sq = sequence_of(a.pb, b);
+  const int n = sq.s1 - sq.s0, rows = n * a.G, tile = slot - first_tile(a.pb, b, a.G, BM);
+  if (tile < 0 || (int64_t)tile * BM >= rows || rows <= few) return;
+  const int r0 = tile * BM;
+  const int before = sq.len - n;                           // position of the sequence's token 0
+  const int last = r0 + BM < rows ? r0 + BM - 1 : rows - 1;
+  const int keys = before + last / a.G + 1;                // that the tile sees
+  const int ranges = keys > part.chunk ? (keys + part.chunk - 1) / part.chunk : 1;
+  if (range >= ranges) return;
+
+  const int bytes = a.D * (int)sizeof(T);
+  int row[QB], seen[QB];
+  u32x4 qf[QB][NC];
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    row[q] = r0 + wave * (16 * QB) + q * 16 + (lane & 15);
+    const int r = row[q] < rows ? row[q] : rows - 1, token = r / a.G;
+    seen[q] = before + token;
+    load_query<NC, EXACT>((const char*)a.Q + ((sq.s0 + token) * a.ldq + (int64_t)(kh * a.G + r % a.G) * a.D) * (int)sizeof(T),
+                          bytes, lane, sign_bits<T>(a.scale), a.scale == 0.f, qf[q]);
+  }
+  // a scale of zero: zero queries, any other scale
+  const float c = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * kLog2e, lag = kLag / c;
+  const int wave_first = r0 + wave * (16 * QB), wave_last = wave_first + 16 * QB - 1;
+  const int seen_lo = before + (wave_first < rows ? wave_first : rows - 1) / a.G;
+  const int seen_hi = before + (wave_last < rows ? wave_last : rows - 1) / a.G;
+
+  const int t0 = range * (part.chunk / TK);
+  const int all = (keys + TK - 1) / TK, t1 = all < t0 + part.chunk / TK ? all : t0 + part.chunk / TK;
+
+  // Loads of a tile: straight to LDS, 16 bytes a lane, RPI rows to an
+  // instruction; the chunk a lane fetches is the one its position holds.  Rows
+  // past the last key repeat it (their scores are masked).
+  auto key_slot = [&](int t) {
+    const int key = t * TK + (lane & (TK - 1));
+    return find_slot(a.pb, b, key < keys ? key : keys - 1);
+  };
+  auto fetch = [&](const Slot& s, int buf) {
+    const uint32_t mine = slot_row(a.pb, s, a.Hk, kh);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int base = (i * 4 + wave) * RPI, r = base + lane / CH;
+      const uint32_t chunk = (uint32_t)(lane % CH) ^ swizzle<RB>(r);
+      const int64_t src = (int64_t)(uint32_t)__shfl((int)mine, r, kWave) * bytes + chunk * 16;
+      if (EXACT || (int)chunk * 16 < bytes) {
+        __builtin_amdgcn_global_load_lds((global_word*)((const char*)a.Kc + src), (lds_word*)&lds[buf][0][base * RB], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_word*)((const char*)a.Vc + src), (lds_word*)&lds[buf][1][base * RB], 16, 0, 0);
+      }
+    }
+  };
+  if constexpr (!EXACT) {
+    // chunks past a row's end are never loaded: zero once
+    for (int i = threadIdx.x * 16; i < (int)sizeof(lds); i += 256 * 16) *(u32x4*)(&lds[0][0][0] + i) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
+
+  uint32_t vb[M::kBases];
+#pragma unroll
+  for (int i = 0; i < M::kBases; ++i) vb[i] = M::template vbase<RB>(lane, i);
+  const uint32_t kb0 = (lane & 15) * RB + (((uint32_t)(lane >> 4) ^ swizzle<RB>(lane & 15)) << 4);
+
+  RowState<DT / 16, QB> rs;
+  rs.clear();
+  uint32_t odd = 0;
+  Slot next = {0, 0};
+  if (t0 < t1) {
+    fetch(key_slot(t0), 0);
+    if (t0 + 1 < t1) next = key_slot(t0 + 1);
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    // this wave's part of tile t has arrived; past the barrier everyone's has,
+    // and everyone is done with tile t - 1
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 1 < t1) fetch(next, buf ^ 1);
+    if (t + 2 < t1) next = key_slot(t + 2);
+    const int k0 = t * TK;
+    if (k0 > seen_hi) continue;
+    const char *kl = lds[buf][0], *vl = lds[buf][1];
+    f32x4 s[NKB][QB];
+#pragma unroll
+    for (int k = 0; k < NKB; ++k) {
+#pragma unroll
+      for (int q = 0; q < QB; ++q) s[k][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ch = 0; ch < NC; ++ch) {
+        const u32x4 kf = *(const u32x4*)(kl + (kb0 ^ (uint32_t)(ch * 64)) + k * 16 * RB);
+#pragma unroll
+        for (int q = 0; q < QB; ++q) s[k][q] = M::mma(kf, qf[q][ch], s[k][q]);
+      }
+    }
+    if (k0 + TK - 1 > seen_lo) {
+      int rel[QB];
+#pragma unroll
+      for (int q = 0; q < QB; ++q) {
+        rel[q] = seen[q] - k0;
+#pragma unroll
+        for (int k = 0; k < NKB; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (16 * k + 4 * (lane >> 4) + i > rel[q]) s[k][q][i] = kNegInf;
+      }
+      softmax_step<NKB, DT / 16, QB>(s, rs, c, lag);
+      weigh<T, RB, true, NKB, DT / 16, QB>(vl, vb, s, rs, odd);
+    } else {
+      softmax_step<NKB, DT / 16, QB>(s, rs, c, lag);
+      weigh<T, RB, false, NKB, DT / 16, QB>(vl, vb, s, rs, odd);
+    }
+  }
+  if (__any(odd != 0)) {
+    // the keys of the masked tiles
+    const int first = (seen_lo + 1) / TK > t0 ? (seen_lo + 1) / TK * TK : t0 * TK;
+#pragma unroll 1
+    for (int k = first; k < t1 * TK && k <= seen_hi; ++k) {
+      bool sees[QB];
+#pragma unroll
+      for (int q = 0; q < QB; ++q) sees[q] = k <= seen[q];
+      add_not_finite<T, DT / 16, QB>((const T*)a.Vc + (int64_t)cache_row(a.pb, b, a.Hk, kh, k) * a.D, a.D, sees, rs);
+    }
+  }
+  finish_rows<T, DT, QB, EXACT>(a, part, rs, row, seen, rows, sq.s0, kh, range, -1, ranges == 1, c, lane);
+}
+
+template <typename T, int DT, int QB>
+static hipError_t launch_tiles(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
+  const int64_t slots = tile_slots(a.pb.N, a.pb.B, a.G, 64 * QB), grid = slots * a.Hk * p.tiles.ranges;
+  if (a.D == DT)
+    hipLaunchKernelGGL((paged_attn_tiles<T, DT, QB, true>), dim3((unsigned)grid), dim3(256), 0, st, a, p.tiles,
+                       p.few, (int)slots);
+  else
+    hipLaunchKernelGGL((paged_attn_tiles<T, DT, QB, false>), dim3((unsigned)grid), dim3(256), 0, st, a, p.tiles,
+                       p.few, (int)slots);
+  return hipGetLastError();
+}
+
+}  // namespace ssn

@@ -6,7 +6,7 @@
 // softmax: for a tile of scores s, m' = max(m, max s), and with a =
 // exp(m - m'), l' = a l + sum exp(s - m'), O' = a O + sum exp(s - m') v; at
 // the end O / l.
-#include "attn_device.h"
+#include "attn_mma.h"
 #include "ssn_launch.h"
 
 namespace ssn {
@@ -70,17 +70,157 @@ __global__ __launch_bounds__(256) void paged_attn_generic(AttnArgs a) {
   }
 }
 
-size_t attention_workspace_bytes(int, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t) {
-  return 0;
+// Joins the partial results of a row's ranges: with M the largest m, O = sum
+// exp2(m - M) O_r / sum exp2(m - M) l_r, in range order.  A block owns a row.
+constexpr int kMaxRanges = 256;
+template <typename T>
+__global__ __launch_bounds__(256) void paged_attn_join(AttnArgs a, AttnPlan plan, int lanes) {
+  __shared__ float red[2][4], weight[kMaxRanges];
+  __shared__ f32x4 part[256];
+  const int tid = threadIdx.x;
+  for (int line = blockIdx.x; line < a.pb.N * a.Hq; line += gridDim.x) {
+    const int token = line / a.Hq, head = line - token * a.Hq, kh = head / a.G;
+    const int b = sequence_of_row(a.pb, token);
+    if (b < 0) continue;
+    const Sequence sq = sequence_of(a.pb, b);
+    if (token >= sq.s1) continue;
+    const int n = sq.s1 - sq.s0, rows = n * a.G, r = (token - sq.s0) * a.G + head % a.G;
+    const bool few = rows <= plan.few;
+    const AttnPart p = few ? plan.rows : plan.tiles;
+    if (p.blocks == 0 || p.ranges <= 1) continue;
+    int keys = sq.len;
+    int64_t at = ((int64_t)b * a.Hk + kh) * (16 * p.blocks) + r;
+    if (!few) {
+      const int bm = 64 * p.blocks, last = (r / bm + 1) * bm - 1;
+      keys = sq.len - n + (last < rows ? last : rows - 1) / a.G + 1;
+      at = line;
+    }
+    if (keys <= p.chunk) continue;
+    const int ranges = (keys + p.chunk - 1) / p.chunk;
+    __syncthreads();      // the line before is done with LDS
+    float m = kNegInf, l = 0.f;
+    if (tid < ranges) {
+      m = p.ml[2 * (tid * p.stage_rows + at)];
+      l = p.ml[2 * (tid * p.stage_rows + at) + 1];
+    }
+    const float wm = wave_max(m);
+    if ((tid & 63) == 0) red[0][tid >> 6] = wm;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    const float w = __builtin_amdgcn_exp2f(m - (top == kNegInf ? 0.f : top));
+    if (tid < ranges) weight[tid] = w;
+    const float ws = wave_sum(tid < ranges ? l * w : 0.f);
+    if ((tid & 63) == 0) red[1][tid >> 6] = ws;
+    __syncthreads();
+    const float sum = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    // `lanes` threads own the row's elements, four each; the groups of them take
+    // the ranges in turn
+    const int e = (tid & (lanes - 1)) * 4;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (e < a.D)
+      for (int g = tid / lanes; g < ranges; g += 256 / lanes)
+        o += *(const f32x4*)(p.o + (g * p.stage_rows + at) * a.D + e) * weight[g];
+    part[tid] = o;
+    __syncthreads();
+    if (tid < lanes && e < a.D) {
+      o = part[tid];
+      for (int g = 1; g < 256 / lanes; ++g) o += part[g * lanes + tid];
+      const bool sees = sq.len - (sq.s1 - token) >= 0;
+      store4((T*)a.O + token * a.ldo + (int64_t)head * a.D + e, o * (sees ? 1.f / sum : 0.f));
+      if (a.lse && tid == 0)
+        a.lse[line] = sees ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f : kNegInf;
+    }
+  }
 }
 
-hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void*, size_t, hipStream_t st) {
-  const int64_t waves = (int64_t)a.pb.N * a.Hq, blocks = (waves + 3) / 4;
-  const unsigned grid = (unsigned)(blocks > (1 << 20) ? (1 << 20) : blocks);
+// How a call is run.  ws: the workspace (NULL: as many bytes as it takes).
+static size_t stage_bytes(const AttnPart& p, int64_t D) {
+  return p.blocks && p.ranges > 1 ? (size_t)p.ranges * (size_t)p.stage_rows * (size_t)(D + 2) * 4 : 0;
+}
+// Ranges for about `want` of them, no more than `fit` bytes hold.
+static void split_keys(AttnPart& p, int64_t want, int64_t unit, int64_t max_len, int64_t D, size_t fit) {
+  const int64_t row_bytes = p.stage_rows * (D + 2) * 4;
+  if (row_bytes > 0 && (size_t)want > fit / (size_t)row_bytes) want = (int64_t)(fit / (size_t)row_bytes);
+  if (want > kMaxRanges) want = kMaxRanges;
+  const int64_t len = max_len > 1 ? max_len : 1;
+  int64_t chunk = want > 1 ? (len + want - 1) / want : len;
+  chunk = (chunk + unit - 1) / unit * unit;
+  p.chunk = (int)chunk;
+  p.ranges = (int)((len + p.chunk - 1) / p.chunk);
+}
+static AttnPlan attention_plan(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
+                               int64_t max_len, size_t ws_bytes) {
+  AttnPlan p = {};
+  const int64_t G = Hq / Hk, most = max_q * G;
+  const bool wide = D > 128;
+  if (most <= 16 || (most <= 32 && !wide)) {
+    p.few = most <= 16 ? 16 : 32;
+  } else {
+    // single tokens among longer chunks, unless all have max_q
+    if (G <= 16 && N != B * max_q) p.few = 16;
+    p.tiles.blocks = (most <= 64 || wide) ? 1 : 2;
+  }
+  p.rows.blocks = (p.few + 15) / 16;
+  p.rows.stage_rows = B * Hk * 16 * p.rows.blocks;
+  p.tiles.stage_rows = N * Hq;
+  if (p.tiles.blocks) {
+    // two blocks to a compute unit, where the rows alone do not give them
+    const int64_t big = p.few ? (N - B + 1 > 1 ? N - B + 1 : 1) : N;
+    const int64_t blocks = (big * G / (64 * p.tiles.blocks) + 1) * Hk;
+    split_keys(p.tiles, blocks >= 512 ? 1 : 512 / blocks, 256, max_len, D, ws_bytes);
+  }
+  if (p.rows.blocks) {
+    const size_t left = ws_bytes - stage_bytes(p.tiles, D);
+    split_keys(p.rows, (2048 + B * Hk - 1) / (B * Hk), 128, max_len, D, left);
+  }
+  return p;
+}
+
+size_t attention_workspace_bytes(int, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
+                                 int64_t max_len) {
+  if (D > 256) return 0;
+  const AttnPlan p = attention_plan(N, B, Hq, Hk, D, max_q, max_len, (size_t)1 << 60);
+  return stage_bytes(p.tiles, D) + stage_bytes(p.rows, D);
+}
+
+// The matrix-core kernels read 16 bytes at a time.
+static bool vector_access(int dtype, const AttnArgs& a) {
+  const int64_t s = dtype == kBF16 ? 2 : 4;
+  const uintptr_t p = (uintptr_t)a.Q | (uintptr_t)a.Kc | (uintptr_t)a.Vc | (uintptr_t)a.O;
+  return a.D <= 256 && (a.D * s) % 16 == 0 && p % 16 == 0 && (a.ldq * s) % 16 == 0 && (a.ldo * s) % 16 == 0;
+}
+
+hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st) {
+  if (!vector_access(dtype, a)) {
+    const int64_t waves = (int64_t)a.pb.N * a.Hq, blocks = (waves + 3) / 4;
+    const unsigned grid = (unsigned)(blocks > (1 << 20) ? (1 << 20) : blocks);
+    if (dtype == kBF16)
+      hipLaunchKernelGGL((paged_attn_generic<uint16_t>), dim3(grid), dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((paged_attn_generic<float>), dim3(grid), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
+  AttnPlan p = attention_plan(a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0);
+  float* at = (float*)ws;
+  for (AttnPart* x : {&p.tiles, &p.rows})
+    if (stage_bytes(*x, a.D)) {
+      x->o = at;
+      x->ml = at + x->ranges * x->stage_rows * a.D;
+      at = x->ml + x->ranges * x->stage_rows * 2;
+    }
+  hipError_t e = hipSuccess;
+  if (p.tiles.blocks) e = dtype == kBF16 ? launch_attn_tiles_bf16(a, p, st) : launch_attn_tiles_f32(a, p, st);
+  if (e == hipSuccess && p.rows.blocks)
+    e = dtype == kBF16 ? launch_attn_rows_bf16(a, p, st) : launch_attn_rows_f32(a, p, st);
+  if (e != hipSuccess || (p.tiles.ranges <= 1 && p.rows.ranges <= 1)) return e;
+  int lanes = 1;
+  while (lanes * 4 < a.D) lanes *= 2;
+  const int64_t lines = (int64_t)a.pb.N * a.Hq;
+  const dim3 grid((unsigned)(lines < (1 << 20) ? lines : (1 << 20)));
   if (dtype == kBF16)
-    hipLaunchKernelGGL((paged_attn_generic<uint16_t>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((paged_attn_join<uint16_t>), grid, dim3(256), 0, st, a, p, lanes);
   else
-    hipLaunchKernelGGL((paged_attn_generic<float>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((paged_attn_join<float>), grid, dim3(256), 0, st, a, p, lanes);
   return hipGetLastError();
 }
 
