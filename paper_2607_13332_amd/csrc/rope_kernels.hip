@@ -5,6 +5,8 @@
 //   r = (mean(x^2) + eps)^-1/2,  n = x r w,  y = rot_p(n)
 // and for g = rot_p^T(dL/dy), h = g w:
 //   dL/dx = r (h - x r mean(h x r)),   dL/dw = sum over rows of g x r
+#include <initializer_list>
+
 #include "attn_device.h"
 #include "ssn_launch.h"
 
@@ -173,6 +175,7 @@ __global__ __launch_bounds__(256) void weight_grad_sum(const float* __restrict__
   float* out = blockIdx.y ? gwk : gwq;
   float s = 0.f;
   if (e < D)
+#pragma unroll 8
     for (int b = g; b < blocks; b += 16) s += ws[((int64_t)b * 2 + blockIdx.y) * D + e];
   part[g][c] = s;
   __syncthreads();
@@ -211,6 +214,364 @@ __global__ __launch_bounds__(256) void kv_append_generic(PagedBatch pb, NormRope
   }
 }
 
+// ---------------------------------------------------------------------------
+// Fast kernels (D = 64, 128, 256; the whole head rotated or none of it; 16-byte
+// alignment).  Memory bounds them: every row is read once and written once.
+//
+// A lane holds two 16-byte chunks of a head, E elements each: E j .. and D/2 +
+// E j .., j its place among the LPH lanes of the head.  With SSN_ROPE_HALVES the
+// two chunks are each other's partners, with SSN_ROPE_PAIRS each is its own, so
+// the rotation never leaves a lane; a head's sums take log2(LPH) exchanges.
+// A wave covers 64 / LPH consecutive heads of a token (a pass; queries, then
+// keys, then values) and keeps to its pass from token to token: its weights and
+// its share of their gradients stay in registers, and the waves of a block read
+// the same rows of the rotation table.
+// ---------------------------------------------------------------------------
+template <typename T>
+struct Chunk {
+  static constexpr int E = 16 / (int)sizeof(T);
+  float v[E];
+  __device__ __forceinline__ void set(u32x4 w) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (E == 8) {
+        v[2 * i] = lo_bf16(w[i]);
+        v[2 * i + 1] = hi_bf16(w[i]);
+      } else {
+        v[i] = __uint_as_float(w[i]);
+      }
+    }
+  }
+  __device__ __forceinline__ u32x4 get() const {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (E == 8) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+      else w[i] = __float_as_uint(v[i]);
+    }
+    return w;
+  }
+  __device__ __forceinline__ void ones() {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = 1.f;
+  }
+};
+
+enum { kNoRotation, kHalves, kPairs };
+
+// Cosines and sines of a lane's pairs: E of each (halves: of the pairs of the
+// two chunks; pairs: E / 2 of the first chunk, then E / 2 of the second).
+template <typename T, int D, int ROT>
+struct Turn {
+  static constexpr int E = Chunk<T>::E;
+  float c[E], s[E];
+  __device__ __forceinline__ void load(const float* __restrict__ row, int j) {
+    if constexpr (ROT == kHalves) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        *(f32x4*)(c + e) = *(const f32x4*)(row + E * j + e);
+        *(f32x4*)(s + e) = *(const f32x4*)(row + D / 2 + E * j + e);
+      }
+    } else if constexpr (ROT == kPairs) {
+      typedef float part __attribute__((ext_vector_type(E / 2)));
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        *(part*)(c + z * E / 2) = *(const part*)(row + z * D / 4 + E / 2 * j);
+        *(part*)(s + z * E / 2) = *(const part*)(row + D / 2 + z * D / 4 + E / 2 * j);
+      }
+    }
+  }
+  // (sign -1: back)
+  __device__ __forceinline__ void apply(Chunk<T>& a, Chunk<T>& b, float sign) const {
+    if constexpr (ROT == kHalves) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float x = a.v[e], y = b.v[e], t = s[e] * sign;
+        a.v[e] = x * c[e] - y * t;
+        b.v[e] = y * c[e] + x * t;
+      }
+    } else if constexpr (ROT == kPairs) {
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) {
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          Chunk<T>& h = z ? b : a;
+          const float x = h.v[2 * e], y = h.v[2 * e + 1], t = s[z * E / 2 + e] * sign, u = c[z * E / 2 + e];
+          h.v[2 * e] = x * u - y * t;
+          h.v[2 * e + 1] = y * u + x * t;
+        }
+      }
+    }
+  }
+};
+
+template <int LPH>
+__device__ __forceinline__ float head_sum(float v) {
+#pragma unroll
+  for (int m = LPH / 2; m >= 1; m >>= 1) v += __shfl_xor(v, m, kWave);
+  return v;
+}
+
+// Waves of a launch: `passes` for each of `slots` tokens; a wave goes on to
+// token + slots.
+struct Spread {
+  int passes, slots;
+  __host__ __device__ int64_t waves() const { return (int64_t)passes * slots; }
+};
+static Spread spread_tokens(int64_t N, int heads, int heads_per_wave, int64_t max_waves) {
+  Spread s;
+  s.passes = (heads + heads_per_wave - 1) / heads_per_wave;
+  const int64_t most = max_waves / s.passes > 1 ? max_waves / s.passes : 1;
+  s.slots = (int)(N < most ? N : most);
+  return s;
+}
+
+// APPEND: keys and values go to their slots of the cache, positions follow
+// from the batch, and the heads of v come after those of k.
+template <typename T, int D, int ROT, bool APPEND>
+__global__ __launch_bounds__(256) void norm_rope_rows(int N, Spread sp, NormRope nr, HeadRows q, HeadRows k,
+                                                      HeadRows v, const T* __restrict__ wq,
+                                                      const T* __restrict__ wk,
+                                                      const int32_t* __restrict__ pos, HeadRows qo,
+                                                      HeadRows ko, PagedBatch pb, T* __restrict__ Kc,
+                                                      T* __restrict__ Vc) {
+  constexpr int E = Chunk<T>::E, LPH = D / (2 * E);
+  const int lane = threadIdx.x & 63;
+  const int id = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (id >= sp.waves()) return;
+  const int pass = id % sp.passes, j = lane % LPH, head = pass * (kWave / LPH) + lane / LPH;
+  const bool isq = head < q.H, isk = !isq && head < q.H + k.H;
+  const bool isv = APPEND && !isq && !isk && head < q.H + 2 * k.H, any = isq || isk || isv;
+  const HeadRows in = isq ? q : (isv ? v : k);
+  const int h = isq ? head : (isv ? head - q.H - k.H : head - q.H);
+  const T* src = (const T*)in.p + h * D + E * j;
+  Chunk<T> wa, wb;
+  wa.ones();
+  wb.ones();
+  const T* w = isq ? wq : wk;
+  if (any && !isv && w) {
+    wa.set(*(const u32x4*)(w + E * j));
+    wb.set(*(const u32x4*)(w + D / 2 + E * j));
+  }
+  for (int i = id / sp.passes; i < N; i += sp.slots) {
+    int p = 0, b = 0;
+    if constexpr (APPEND) {
+      b = sequence_of_row(pb, i);
+      if (b < 0) continue;
+      const Sequence sq = sequence_of(pb, b);
+      p = sq.len - (sq.s1 - i);
+      if (i >= sq.s1 || p < 0) continue;
+    } else if constexpr (ROT != kNoRotation) {
+      p = pos[i];
+    }
+    u32x4 xa = {0, 0, 0, 0}, xb = {0, 0, 0, 0};
+    if (any) {
+      xa = __builtin_nontemporal_load((const u32x4*)(src + i * in.ld));
+      xb = __builtin_nontemporal_load((const u32x4*)(src + i * in.ld + D / 2));
+    }
+    Turn<T, D, ROT> turn;
+    if constexpr (ROT != kNoRotation) turn.load(nr.table + (int64_t)clampi(p, 0, nr.P - 1) * D, j);
+    T* dst;
+    if (isq) dst = (T*)qo.p + i * qo.ld + h * D;
+    else if constexpr (APPEND) dst = (isv ? Vc : Kc) + (int64_t)cache_row(pb, b, k.H, any ? h : 0, p) * D;
+    else dst = (T*)ko.p + i * ko.ld + h * D;
+    if (!isv) {
+      Chunk<T> a, c;
+      a.set(xa);
+      c.set(xb);
+      if (nr.eps >= 0.f) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) ss += a.v[e] * a.v[e] + c.v[e] * c.v[e];
+        const float r = rsqrtf(head_sum<LPH>(ss) * (1.f / D) + nr.eps);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          a.v[e] *= r * wa.v[e];
+          c.v[e] *= r * wb.v[e];
+        }
+      }
+      turn.apply(a, c, 1.f);
+      xa = a.get();
+      xb = c.get();
+    }
+    if (any) {
+      *(u32x4*)(dst + E * j) = xa;
+      *(u32x4*)(dst + D / 2 + E * j) = xb;
+    }
+  }
+}
+
+constexpr int kBackWaves = 8;         // of a block
+template <typename T, int D, int ROT>
+__global__ __launch_bounds__(64 * kBackWaves) void norm_rope_backward_rows(
+    int N, Spread sp, NormRope nr, HeadRows q, HeadRows k, const T* __restrict__ wq, const T* __restrict__ wk,
+    const int32_t* __restrict__ pos, HeadRows gq, HeadRows gk, HeadRows gqi, HeadRows gki,
+    float* __restrict__ ws) {
+  constexpr int E = Chunk<T>::E, LPH = D / (2 * E);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int id = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kBackWaves + wave));
+  const int pass = id % sp.passes, j = lane % LPH, head = pass * (kWave / LPH) + lane / LPH;
+  const bool isq = head < q.H, any = head < q.H + k.H;
+  const int h = isq ? head : head - q.H;
+  const HeadRows in = isq ? q : k, gin = isq ? gq : gk, out = isq ? gqi : gki;
+  const T* src = (const T*)in.p + h * D + E * j;
+  const T* gsrc = (const T*)gin.p + h * D + E * j;
+  T* dst = (T*)out.p + h * D + E * j;
+  Chunk<T> wa, wb, ga, gb;              // ga, gb: shares of dL/dw
+  wa.ones();
+  wb.ones();
+  const T* w = isq ? wq : wk;
+  if (any && w) {
+    wa.set(*(const u32x4*)(w + E * j));
+    wb.set(*(const u32x4*)(w + D / 2 + E * j));
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) ga.v[e] = gb.v[e] = 0.f;
+  const int first = id < sp.waves() ? id / sp.passes : N;
+  for (int i = first; i < N; i += sp.slots) {
+    u32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, y[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (any) {
+      x[0] = __builtin_nontemporal_load((const u32x4*)(src + i * in.ld));
+      x[1] = __builtin_nontemporal_load((const u32x4*)(src + i * in.ld + D / 2));
+      y[0] = __builtin_nontemporal_load((const u32x4*)(gsrc + i * gin.ld));
+      y[1] = __builtin_nontemporal_load((const u32x4*)(gsrc + i * gin.ld + D / 2));
+    }
+    Turn<T, D, ROT> turn;
+    if constexpr (ROT != kNoRotation) turn.load(nr.table + (int64_t)clampi(pos[i], 0, nr.P - 1) * D, j);
+    Chunk<T> xa, xb, a, b;
+    xa.set(x[0]);
+    xb.set(x[1]);
+    a.set(y[0]);
+    b.set(y[1]);
+    turn.apply(a, b, -1.f);
+    if (nr.eps >= 0.f) {
+      float ss = 0.f, dot = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        ss += xa.v[e] * xa.v[e] + xb.v[e] * xb.v[e];
+        dot += a.v[e] * wa.v[e] * xa.v[e] + b.v[e] * wb.v[e] * xb.v[e];
+      }
+      const float r = rsqrtf(head_sum<LPH>(ss) * (1.f / D) + nr.eps);
+      // x r times the mean of h x r, times r
+      const float m = head_sum<LPH>(dot) * (1.f / D) * r * r * r;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        ga.v[e] += a.v[e] * (xa.v[e] * r);
+        gb.v[e] += b.v[e] * (xb.v[e] * r);
+        a.v[e] = a.v[e] * wa.v[e] * r - xa.v[e] * m;
+        b.v[e] = b.v[e] * wb.v[e] * r - xb.v[e] * m;
+      }
+    }
+    if (any) {
+      *(u32x4*)(dst + i * out.ld) = a.get();
+      *(u32x4*)(dst + i * out.ld + D / 2) = b.get();
+    }
+  }
+  if (!ws) return;
+  // the heads of a wave, then the waves of a block in order
+  __shared__ float part[kBackWaves][2][D];
+#pragma unroll
+  for (int z = 0; z < 2; ++z)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float s = (isq == (z == 0)) ? ga.v[e] : 0.f, t = (isq == (z == 0)) ? gb.v[e] : 0.f;
+#pragma unroll
+      for (int m = LPH; m < kWave; m <<= 1) {
+        s += __shfl_xor(s, m, kWave);
+        t += __shfl_xor(t, m, kWave);
+      }
+      if (lane < LPH) {
+        part[wave][z][E * j + e] = s;
+        part[wave][z][D / 2 + E * j + e] = t;
+      }
+    }
+  __syncthreads();
+  for (int e = threadIdx.x; e < 2 * D; e += 64 * kBackWaves) {
+    float s = 0.f;
+#pragma unroll
+    for (int m = 0; m < kBackWaves; ++m) s += part[m][e / D][e % D];
+    ws[(int64_t)blockIdx.x * 2 * D + e] = s;
+  }
+}
+
+static bool aligned16(const HeadRows& r, int64_t s) {
+  return r.H == 0 || ((uintptr_t)r.p % 16 == 0 && (r.ld * s) % 16 == 0);
+}
+static bool fast_heads(int dtype, const NormRope& nr, std::initializer_list<HeadRows> rows,
+                       std::initializer_list<const void*> ptrs) {
+  if ((nr.D != 64 && nr.D != 128 && nr.D != 256) || (nr.R != 0 && nr.R != nr.D)) return false;
+  for (const HeadRows& r : rows)
+    if (!aligned16(r, dtype == kBF16 ? 2 : 4)) return false;
+  for (const void* p : ptrs)
+    if ((uintptr_t)p % 16) return false;
+  return (uintptr_t)nr.table % 16 == 0;
+}
+
+struct RowsLaunch {
+  int64_t N;
+  NormRope nr;
+  HeadRows q, k, v;
+  const void *wq, *wk;
+  const int32_t* pos;
+  HeadRows qo, ko;
+  PagedBatch pb;
+  void *Kc, *Vc;
+  bool append;
+  hipStream_t st;
+};
+template <typename T, int D, int ROT, bool APPEND>
+static hipError_t launch_rows_kernel(const RowsLaunch& a) {
+  const Spread sp = spread_tokens(a.N, a.q.H + (APPEND ? 2 : 1) * a.k.H, kWave * 2 * Chunk<T>::E / D, 32768);
+  hipLaunchKernelGGL((norm_rope_rows<T, D, ROT, APPEND>), dim3((unsigned)((sp.waves() + 3) / 4)), dim3(256), 0,
+                     a.st, (int)a.N, sp, a.nr, a.q, a.k, a.v, (const T*)a.wq, (const T*)a.wk, a.pos, a.qo, a.ko,
+                     a.pb, (T*)a.Kc, (T*)a.Vc);
+  return hipGetLastError();
+}
+template <typename T, int D, int ROT>
+static hipError_t launch_rows_append(const RowsLaunch& a) {
+  return a.append ? launch_rows_kernel<T, D, ROT, true>(a) : launch_rows_kernel<T, D, ROT, false>(a);
+}
+template <typename T, int D>
+static hipError_t launch_rows_rot(const RowsLaunch& a) {
+  if (!a.nr.R) return launch_rows_append<T, D, kNoRotation>(a);
+  return a.nr.pairs ? launch_rows_append<T, D, kPairs>(a) : launch_rows_append<T, D, kHalves>(a);
+}
+template <typename T>
+static hipError_t launch_rows_fast(const RowsLaunch& a) {
+  if (a.nr.D == 64) return launch_rows_rot<T, 64>(a);
+  return a.nr.D == 128 ? launch_rows_rot<T, 128>(a) : launch_rows_rot<T, 256>(a);
+}
+
+struct BackLaunch {
+  int64_t N;
+  NormRope nr;
+  HeadRows q, k;
+  const void *wq, *wk;
+  const int32_t* pos;
+  HeadRows gq, gk, gqi, gki;
+  float* ws;
+  int blocks;
+  hipStream_t st;
+};
+template <typename T, int D, int ROT>
+static hipError_t launch_back_kernel(const BackLaunch& a) {
+  const Spread sp = spread_tokens(a.N, a.q.H + a.k.H, kWave * 2 * Chunk<T>::E / D, (int64_t)a.blocks * kBackWaves);
+  hipLaunchKernelGGL((norm_rope_backward_rows<T, D, ROT>), dim3(a.blocks), dim3(64 * kBackWaves), 0, a.st,
+                     (int)a.N, sp, a.nr, a.q, a.k, (const T*)a.wq, (const T*)a.wk, a.pos, a.gq, a.gk, a.gqi, a.gki,
+                     a.ws);
+  return hipGetLastError();
+}
+template <typename T, int D>
+static hipError_t launch_back_rot(const BackLaunch& a) {
+  if (!a.nr.R) return launch_back_kernel<T, D, kNoRotation>(a);
+  return a.nr.pairs ? launch_back_kernel<T, D, kPairs>(a) : launch_back_kernel<T, D, kHalves>(a);
+}
+template <typename T>
+static hipError_t launch_back_fast(const BackLaunch& a) {
+  if (a.nr.D == 64) return launch_back_rot<T, 64>(a);
+  return a.nr.D == 128 ? launch_back_rot<T, 128>(a) : launch_back_rot<T, 256>(a);
+}
+
 static unsigned wave_blocks(int64_t waves) {
   const int64_t b = (waves + 3) / 4;
   return (unsigned)(b < 1 ? 1 : (b > (1 << 20) ? (1 << 20) : b));
@@ -219,6 +580,10 @@ static unsigned wave_blocks(int64_t waves) {
 hipError_t launch_norm_rope(int dtype, int64_t N, const NormRope& nr, HeadRows q, HeadRows k,
                             const void* wq, const void* wk, const int32_t* pos, HeadRows qo, HeadRows ko,
                             hipStream_t st) {
+  if (fast_heads(dtype, nr, {q, k, qo, ko}, {wq, wk})) {
+    const RowsLaunch a = {N, nr, q, k, HeadRows{}, wq, wk, pos, qo, ko, PagedBatch{}, nullptr, nullptr, false, st};
+    return dtype == kBF16 ? launch_rows_fast<uint16_t>(a) : launch_rows_fast<float>(a);
+  }
   const unsigned blocks = wave_blocks(N * (q.H + k.H));
   if (dtype == kBF16)
     hipLaunchKernelGGL((norm_rope_generic<uint16_t>), dim3(blocks), dim3(256), 0, st, (int)N, nr, q, k,
@@ -229,9 +594,11 @@ hipError_t launch_norm_rope(int dtype, int64_t N, const NormRope& nr, HeadRows q
   return hipGetLastError();
 }
 
+// Enough waves for two blocks of 8 on every compute unit, and few enough
+// partial sums that adding them costs nothing.
 int norm_rope_backward_blocks(int64_t N, int64_t heads) {
-  const int64_t b = (N * heads + 31) / 32;      // 8 heads a wave at least
-  return (int)(b < 1 ? 1 : (b > 2048 ? 2048 : b));
+  const int64_t b = (N * heads + 31) / 32;
+  return (int)(b < 1 ? 1 : (b > 512 ? 512 : b));
 }
 
 hipError_t launch_norm_rope_backward(int dtype, int64_t N, const NormRope& nr, HeadRows q, HeadRows k,
@@ -240,7 +607,11 @@ hipError_t launch_norm_rope_backward(int dtype, int64_t N, const NormRope& nr, H
                                      float* ws, hipStream_t st) {
   const int blocks = N ? norm_rope_backward_blocks(N, q.H + k.H) : 0;
   float* stage = (gwq || gwk) ? ws : nullptr;
-  if (blocks && dtype == kBF16)
+  if (blocks && fast_heads(dtype, nr, {q, k, gq, gk, gqi, gki}, {wq, wk})) {
+    const BackLaunch a = {N, nr, q, k, wq, wk, pos, gq, gk, gqi, gki, stage, blocks, st};
+    const hipError_t e = dtype == kBF16 ? launch_back_fast<uint16_t>(a) : launch_back_fast<float>(a);
+    if (e != hipSuccess) return e;
+  } else if (blocks && dtype == kBF16)
     hipLaunchKernelGGL((norm_rope_backward_generic<uint16_t>), dim3(blocks), dim3(256), 0, st, (int)N, nr,
                        q, k, (const uint16_t*)wq, (const uint16_t*)wk, pos, gq, gk, gqi, gki, stage);
   else if (blocks)
@@ -255,6 +626,10 @@ hipError_t launch_norm_rope_backward(int dtype, int64_t N, const NormRope& nr, H
 hipError_t launch_kv_append(int dtype, const PagedBatch& pb, const NormRope& nr, HeadRows q, HeadRows k,
                             HeadRows v, const void* wq, const void* wk, void* Kc, void* Vc, HeadRows qo,
                             hipStream_t st) {
+  if (fast_heads(dtype, nr, {q, k, v, qo}, {wq, wk, Kc, Vc})) {
+    const RowsLaunch a = {pb.N, nr, q, k, v, wq, wk, nullptr, qo, HeadRows{}, pb, Kc, Vc, true, st};
+    return dtype == kBF16 ? launch_rows_fast<uint16_t>(a) : launch_rows_fast<float>(a);
+  }
   const unsigned blocks = wave_blocks((int64_t)pb.N * (q.H + 2 * k.H));
   if (dtype == kBF16)
     hipLaunchKernelGGL((kv_append_generic<uint16_t>), dim3(blocks), dim3(256), 0, st, pb, nr, q, k, v,
