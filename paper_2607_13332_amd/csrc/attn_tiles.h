@@ -108,8 +108,7 @@ __global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void pag
   }
   // a scale of zero: zero queries, any other scale
   const float c = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * kLog2e, lag = kLag / c;
-  const int wave_first = r0 + wave * (16 * QB), wave_last = wave_first + 16 * QB - 1;
-  const int seen_lo = before + (wave_first < rows ? wave_first : rows - 1) / a.G;
+  const int wave_last = r0 + (wave + 1) * (16 * QB) - 1;
   const int seen_hi = before + (wave_last < rows ? wave_last : rows - 1) / a.G;
 
   const int t0 = range * (part.chunk / TK);
@@ -154,18 +153,15 @@ __global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void pag
     fetch(key_slot(t0), 0);
     if (t0 + 1 < t1) next = key_slot(t0 + 1);
   }
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
+  auto arrive = [&](int t) {
     // this wave's part of tile t has arrived; past the barrier everyone's has,
     // and everyone is done with tile t - 1
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (t + 1 < t1) fetch(next, buf ^ 1);
+    if (t + 1 < t1) fetch(next, (t + 1 - t0) & 1);
     if (t + 2 < t1) next = key_slot(t + 2);
-    const int k0 = t * TK;
-    if (k0 > seen_hi) continue;
-    const char *kl = lds[buf][0], *vl = lds[buf][1];
-    f32x4 s[NKB][QB];
+  };
+  auto scores = [&](const char* kl, f32x4 (&s)[NKB][QB]) {
 #pragma unroll
     for (int k = 0; k < NKB; ++k) {
 #pragma unroll
@@ -177,29 +173,39 @@ __global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void pag
         for (int q = 0; q < QB; ++q) s[k][q] = M::mma(kf, qf[q][ch], s[k][q]);
       }
     }
-    if (k0 + TK - 1 > seen_lo) {
-      int rel[QB];
+  };
+  // Tiles that every row of the block sees, then the others.  (Two loops: one
+  // with both cases keeps O in two sets of registers.)
+  const int open = (before + r0 / a.G + 1) / TK, t_open = open < t0 ? t0 : (open < t1 ? open : t1);
+  int t = t0;
+  for (; t < t_open; ++t) {
+    arrive(t);
+    const int buf = (t - t0) & 1;
+    f32x4 s[NKB][QB];
+    scores(lds[buf][0], s);
+    softmax_step<NKB, DT / 16, QB>(s, rs, c, lag);
+    weigh<T, RB, false, NKB, DT / 16, QB>(lds[buf][1], vb, s, rs, odd);
+  }
+  for (; t < t1; ++t) {
+    arrive(t);
+    const int buf = (t - t0) & 1, k0 = t * TK;
+    if (k0 > seen_hi) continue;
+    f32x4 s[NKB][QB];
+    scores(lds[buf][0], s);
 #pragma unroll
-      for (int q = 0; q < QB; ++q) {
-        rel[q] = seen[q] - k0;
+    for (int q = 0; q < QB; ++q)
 #pragma unroll
-        for (int k = 0; k < NKB; ++k)
+      for (int k = 0; k < NKB; ++k)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (16 * k + 4 * (lane >> 4) + i > rel[q]) s[k][q][i] = kNegInf;
-      }
-      softmax_step<NKB, DT / 16, QB>(s, rs, c, lag);
-      weigh<T, RB, true, NKB, DT / 16, QB>(vl, vb, s, rs, odd);
-    } else {
-      softmax_step<NKB, DT / 16, QB>(s, rs, c, lag);
-      weigh<T, RB, false, NKB, DT / 16, QB>(vl, vb, s, rs, odd);
-    }
+        for (int i = 0; i < 4; ++i)
+          if (16 * k + 4 * (lane >> 4) + i > seen[q] - k0) s[k][q][i] = kNegInf;
+    softmax_step<NKB, DT / 16, QB>(s, rs, c, lag);
+    weigh<T, RB, true, NKB, DT / 16, QB>(lds[buf][1], vb, s, rs, odd);
   }
   if (__any(odd != 0)) {
     // the keys of the masked tiles
-    const int first = (seen_lo + 1) / TK > t0 ? (seen_lo + 1) / TK * TK : t0 * TK;
 #pragma unroll 1
-    for (int k = first; k < t1 * TK && k <= seen_hi; ++k) {
+    for (int k = t_open * TK; k < t1 * TK && k <= seen_hi; ++k) {
       bool sees[QB];
 #pragma unroll
       for (int q = 0; q < QB; ++q) sees[q] = k <= seen[q];

@@ -71,66 +71,105 @@ __global__ __launch_bounds__(256) void paged_attn_generic(AttnArgs a) {
 }
 
 // Joins the partial results of a row's ranges: with M the largest m, O = sum
-// exp2(m - M) O_r / sum exp2(m - M) l_r, in range order.  A block owns a row.
-constexpr int kMaxRanges = 256;
-template <typename T>
-__global__ __launch_bounds__(256) void paged_attn_join(AttnArgs a, AttnPlan plan, int lanes) {
-  __shared__ float red[2][4], weight[kMaxRanges];
-  __shared__ f32x4 part[256];
-  const int tid = threadIdx.x;
-  for (int line = blockIdx.x; line < a.pb.N * a.Hq; line += gridDim.x) {
-    const int token = line / a.Hq, head = line - token * a.Hq, kh = head / a.G;
-    const int b = sequence_of_row(a.pb, token);
-    if (b < 0) continue;
-    const Sequence sq = sequence_of(a.pb, b);
-    if (token >= sq.s1) continue;
-    const int n = sq.s1 - sq.s0, rows = n * a.G, r = (token - sq.s0) * a.G + head % a.G;
-    const bool few = rows <= plan.few;
-    const AttnPart p = few ? plan.rows : plan.tiles;
-    if (p.blocks == 0 || p.ranges <= 1) continue;
-    int keys = sq.len;
-    int64_t at = ((int64_t)b * a.Hk + kh) * (16 * p.blocks) + r;
-    if (!few) {
-      const int bm = 64 * p.blocks, last = (r / bm + 1) * bm - 1;
-      keys = sq.len - n + (last < rows ? last : rows - 1) / a.G + 1;
-      at = line;
-    }
-    if (keys <= p.chunk) continue;
-    const int ranges = (keys + p.chunk - 1) / p.chunk;
-    __syncthreads();      // the line before is done with LDS
-    float m = kNegInf, l = 0.f;
-    if (tid < ranges) {
-      m = p.ml[2 * (tid * p.stage_rows + at)];
-      l = p.ml[2 * (tid * p.stage_rows + at) + 1];
-    }
-    const float wm = wave_max(m);
-    if ((tid & 63) == 0) red[0][tid >> 6] = wm;
-    __syncthreads();
-    const float top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-    const float w = __builtin_amdgcn_exp2f(m - (top == kNegInf ? 0.f : top));
-    if (tid < ranges) weight[tid] = w;
-    const float ws = wave_sum(tid < ranges ? l * w : 0.f);
-    if ((tid & 63) == 0) red[1][tid >> 6] = ws;
-    __syncthreads();
-    const float sum = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
-    // `lanes` threads own the row's elements, four each; the groups of them take
-    // the ranges in turn
-    const int e = (tid & (lanes - 1)) * 4;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    if (e < a.D)
-      for (int g = tid / lanes; g < ranges; g += 256 / lanes)
-        o += *(const f32x4*)(p.o + (g * p.stage_rows + at) * a.D + e) * weight[g];
-    part[tid] = o;
-    __syncthreads();
-    if (tid < lanes && e < a.D) {
-      o = part[tid];
-      for (int g = 1; g < 256 / lanes; ++g) o += part[g * lanes + tid];
-      const bool sees = sq.len - (sq.s1 - token) >= 0;
-      store4((T*)a.O + token * a.ldo + (int64_t)head * a.D + e, o * (sees ? 1.f / sum : 0.f));
-      if (a.lse && tid == 0)
-        a.lse[line] = sees ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f : kNegInf;
-    }
+// exp2(m - M) O_r / sum exp2(m - M) l_r, in a fixed order.  A wave owns a row:
+// lane i the (m, l) of ranges i, i + 64, ..; then `lanes` lanes the row's
+// elements, four each, the groups of them the ranges in turn.
+constexpr int kMaxRanges = 256, kRangeChunks = kMaxRanges / kWave;
+
+// Row r of sequence b and key head kh, its partial results at `at`.
+struct JoinRow {
+  int b, kh, r, ranges;
+  int64_t at;
+  Sequence sq;
+};
+// Line `line` of the rows kernel's stage, or of the batch's (token, head) pairs.
+template <bool FEW>
+__device__ __forceinline__ bool join_row(const AttnArgs& a, const AttnPart& p, int few, int line, JoinRow& j) {
+  if constexpr (FEW) {
+    const int per = 16 * p.blocks;
+    j.r = line % per;
+    j.kh = line / per % a.Hk;
+    j.b = line / per / a.Hk;
+  } else {
+    const int token = line / a.Hq, head = line - token * a.Hq;
+    j.b = sequence_of_row(a.pb, token);
+    if (j.b < 0) return false;
+    j.kh = head / a.G;
+    j.r = (token - clampi(a.pb.starts[j.b], 0, a.pb.N)) * a.G + head % a.G;
   }
+  j.sq = sequence_of(a.pb, j.b);
+  const int n = j.sq.s1 - j.sq.s0, rows = n * a.G;
+  if (j.r >= rows || (rows <= few) != FEW) return false;
+  int keys = j.sq.len;
+  if constexpr (!FEW) {
+    const int bm = 64 * p.blocks, last = (j.r / bm + 1) * bm - 1;
+    keys = j.sq.len - n + (last < rows ? last : rows - 1) / a.G + 1;
+  }
+  j.at = line;
+  j.ranges = keys > p.chunk ? (keys + p.chunk - 1) / p.chunk : 1;
+  return j.ranges > 1;
+}
+
+template <typename T, bool FEW>
+__global__ __launch_bounds__(256) void paged_attn_join(AttnArgs a, AttnPart p, int few, int lines, int lanes) {
+  const int lane = threadIdx.x & 63;
+  for (int line = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6))); line < lines;
+       line += gridDim.x * 4) {
+    JoinRow j;
+    if (!join_row<FEW>(a, p, few, line, j)) continue;
+    float w[kRangeChunks], sum = 0.f, top = kNegInf;
+#pragma unroll
+    for (int c = 0; c < kRangeChunks; ++c) {
+      w[c] = kNegInf;
+      if (c * kWave + lane < j.ranges) w[c] = p.ml[2 * ((c * kWave + lane) * p.stage_rows + j.at)];
+      top = fmaxf(top, w[c]);
+    }
+    top = wave_max(top);
+#pragma unroll
+    for (int c = 0; c < kRangeChunks; ++c)
+      if (c * kWave + lane < j.ranges) {
+        w[c] = __builtin_amdgcn_exp2f(w[c] - (top == kNegInf ? 0.f : top));
+        sum += p.ml[2 * ((c * kWave + lane) * p.stage_rows + j.at) + 1] * w[c];
+      }
+    sum = wave_sum(sum);
+    const int e = (lane & (lanes - 1)) * 4, groups = kWave / lanes;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < kRangeChunks; ++c) {
+      const int n = j.ranges - c * kWave < kWave ? j.ranges - c * kWave : kWave;
+#pragma unroll 4
+      for (int g = 0; g < n; g += groups) {
+        const int mine = g + lane / lanes;
+        const float weight = __shfl(w[c], mine & 63, kWave);
+        if (mine < n && e < a.D)
+          o += *(const f32x4*)(p.o + ((c * kWave + mine) * p.stage_rows + j.at) * a.D + e) * weight;
+      }
+    }
+    for (int m = lanes; m < kWave; m <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m, kWave);
+    const int64_t token = j.sq.s0 + j.r / a.G;
+    const int head = j.kh * a.G + j.r % a.G;
+    const bool sees = j.sq.len - (j.sq.s1 - (int)token) >= 0;
+    if (lane < lanes && e < a.D)
+      store4((T*)a.O + token * a.ldo + (int64_t)head * a.D + e, o * (sees ? 1.f / sum : 0.f));
+    if (a.lse && lane == 0)
+      a.lse[token * a.Hq + head] = sees ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f : kNegInf;
+  }
+}
+
+template <bool FEW>
+static hipError_t launch_join(int dtype, const AttnArgs& a, const AttnPart& p, int few, hipStream_t st) {
+  if (p.blocks == 0 || p.ranges <= 1) return hipSuccess;
+  int lanes = 1;
+  while (lanes * 4 < a.D) lanes *= 2;
+  const int lines = (int)p.stage_rows;
+  const dim3 grid((unsigned)((lines + 3) / 4 < (1 << 20) ? (lines + 3) / 4 : (1 << 20)));
+  if (dtype == kBF16)
+    hipLaunchKernelGGL((paged_attn_join<uint16_t, FEW>), grid, dim3(256), 0, st, a, p, few, lines, lanes);
+  else
+    hipLaunchKernelGGL((paged_attn_join<float, FEW>), grid, dim3(256), 0, st, a, p, few, lines, lanes);
+  return hipGetLastError();
 }
 
 // How a call is run.  ws: the workspace (NULL: as many bytes as it takes).
@@ -171,7 +210,8 @@ static AttnPlan attention_plan(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int
   }
   if (p.rows.blocks) {
     const size_t left = ws_bytes - stage_bytes(p.tiles, D);
-    split_keys(p.rows, (2048 + B * Hk - 1) / (B * Hk), 128, max_len, D, left);
+    const int64_t pairs = B * Hk, full = 512 / pairs, want = (2048 + pairs - 1) / pairs;
+    split_keys(p.rows, want > 64 && want > full ? (full > 64 ? full : 64) : want, 128, max_len, D, left);
   }
   return p;
 }
@@ -212,16 +252,8 @@ hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void* ws, size_t
   if (p.tiles.blocks) e = dtype == kBF16 ? launch_attn_tiles_bf16(a, p, st) : launch_attn_tiles_f32(a, p, st);
   if (e == hipSuccess && p.rows.blocks)
     e = dtype == kBF16 ? launch_attn_rows_bf16(a, p, st) : launch_attn_rows_f32(a, p, st);
-  if (e != hipSuccess || (p.tiles.ranges <= 1 && p.rows.ranges <= 1)) return e;
-  int lanes = 1;
-  while (lanes * 4 < a.D) lanes *= 2;
-  const int64_t lines = (int64_t)a.pb.N * a.Hq;
-  const dim3 grid((unsigned)(lines < (1 << 20) ? lines : (1 << 20)));
-  if (dtype == kBF16)
-    hipLaunchKernelGGL((paged_attn_join<uint16_t>), grid, dim3(256), 0, st, a, p, lanes);
-  else
-    hipLaunchKernelGGL((paged_attn_join<float>), grid, dim3(256), 0, st, a, p, lanes);
-  return hipGetLastError();
+  if (e == hipSuccess) e = launch_join<false>(dtype, a, p.tiles, p.few, st);
+  return e == hipSuccess ? launch_join<true>(dtype, a, p.rows, p.few, st) : e;
 }
 
 }  // namespace ssn
