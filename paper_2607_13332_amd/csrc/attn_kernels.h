@@ -1,0 +1,70 @@
+// The paged attention's kernels: tiles, rows, or both in one launch.
+#pragma once
+
+#include "attn_rows.h"
+#include "attn_tiles.h"
+
+namespace ssn {
+
+// Blocks of a compute unit: two where 256 registers hold a wave's rows (and, in
+// the rows kernel, its keys and values).
+template <typename T, int DT, int QB>
+constexpr int rows_blocks() { return DT * (int)sizeof(T) * QB <= 256 ? 2 : 1; }
+template <typename T, int DT>
+constexpr int tiles_blocks() { return DT * (int)sizeof(T) <= 512 ? 2 : 1; }
+
+template <typename T, int DT, int QB, bool EXACT>
+__global__ __launch_bounds__(256, (rows_blocks<T, DT, QB>())) void paged_attn_rows(AttnArgs a, AttnPart part,
+                                                                                  int few) {
+  __shared__ __align__(1024) char lds[rows_lds<T, DT, QB>()];
+  rows_block<T, DT, QB, EXACT>(a, part, few, blockIdx.x, lds);
+}
+
+template <typename T, int DT, int QB, bool EXACT>
+__global__ __launch_bounds__(256, (tiles_blocks<T, DT>())) void paged_attn_tiles(AttnArgs a, AttnPart part,
+                                                                                 int few, int slots) {
+  __shared__ __align__(1024) char lds[tiles_lds<T, DT>()];
+  tiles_block<T, DT, QB, EXACT>(a, part, few, slots, blockIdx.x, lds);
+}
+
+// Both: the tiles' blocks are bound by the matrix cores, the rows' by memory, so
+// they go out in alternate rounds of one block to a compute unit.
+template <typename T, int DT>
+constexpr int both_blocks() { return rows_blocks<T, DT, 1>() < tiles_blocks<T, DT>() ? rows_blocks<T, DT, 1>() : tiles_blocks<T, DT>(); }
+template <typename T, int DT, int QB, bool EXACT>
+__global__ __launch_bounds__(256, (both_blocks<T, DT>())) void paged_attn_both(AttnArgs a, AttnPlan p, int slots,
+                                                                                int tiles, int rows) {
+  constexpr int kLds = tiles_lds<T, DT>() > rows_lds<T, DT, 1>() ? tiles_lds<T, DT>() : rows_lds<T, DT, 1>();
+  __shared__ __align__(1024) char lds[kLds];
+  const int id = blockIdx.x, round = id / kUnits, at = id % kUnits;
+  const int less = (tiles < rows ? tiles : rows) / kUnits;     // whole rounds of both
+  const bool tile = round < 2 * less ? !(round & 1) : id - less * kUnits < tiles;
+  const int t = round < 2 * less ? round / 2 * kUnits + at : (tile ? id - less * kUnits : id - tiles);
+  if (tile) tiles_block<T, DT, QB, EXACT>(a, p.tiles, p.few, slots, t, lds);
+  else rows_block<T, DT, 1, EXACT>(a, p.rows, p.few, t, lds);
+}
+
+template <typename T, int DT, int QB, bool EXACT>
+static hipError_t launch_rows(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
+  const int64_t grid = (int64_t)a.pb.B * a.Hk * p.rows.ranges;
+  hipLaunchKernelGGL((paged_attn_rows<T, DT, QB, EXACT>), dim3((unsigned)grid), dim3(256), 0, st, a, p.rows, p.few);
+  return hipGetLastError();
+}
+template <typename T, int DT, int QB, bool EXACT>
+static hipError_t launch_tiles(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
+  const int64_t slots = tile_slots(a.pb.N, a.pb.B, a.G, 64 * QB), tiles = slots * a.Hk * p.tiles.ranges;
+  if (p.rows.blocks) {
+    const int64_t rows = (int64_t)a.pb.B * a.Hk * p.rows.ranges;
+    hipLaunchKernelGGL((paged_attn_both<T, DT, QB, EXACT>), dim3((unsigned)(tiles + rows)), dim3(256), 0, st, a, p,
+                       (int)slots, (int)tiles, (int)rows);
+  } else {
+    hipLaunchKernelGGL((paged_attn_tiles<T, DT, QB, EXACT>), dim3((unsigned)tiles), dim3(256), 0, st, a, p.tiles,
+                       p.few, (int)slots);
+  }
+  return hipGetLastError();
+}
+// For a.D == DT and for the heads padded to DT in registers and LDS.
+#define SSN_ATTN_EXACT(launch, T, DT, QB) \
+  (a.D == DT ? launch<T, DT, QB, true>(a, p, st) : launch<T, DT, QB, false>(a, p, st))
+
+}  // namespace ssn

@@ -102,7 +102,7 @@ struct Mma<float> {
   }
 };
 
-// What a wave keeps of 16 QB rows: m (the largest score the sums are taken
+// What a wave keeps of 16 QB rows: m (the score the sums are taken
 // against, before the scale; the same in the four lanes of a column), l (this
 // lane's share of the sum of exp2((s - m) c)) and O^T.
 template <int DT16, int QB>
@@ -120,71 +120,78 @@ struct RowState {
   }
 };
 
-// Scores to probabilities, in place: s = exp2((s - m) c), l and (if the
-// maximum moves) O rescaled.  m follows the true maximum only when that passes
-// it by kLag in the exponent: the sums are exact for any m, a probability is at
-// most 2^kLag, and most tiles skip the rescaling of O.
-constexpr float kLag = 8.f;
-template <int NKB, int DT16, int QB>
-__device__ __forceinline__ void softmax_step(f32x4 (&s)[NKB][QB], RowState<DT16, QB>& st, float c, float lag) {
-  bool moved = false;
-  float mx[QB];
+// Scores to probabilities exp2((s - m) c), as the B operands of the second
+// product, and l += their sum.  m does not follow the maximum: the sums are the
+// same against any m, so a row's moves (and its l and O are rescaled) only where
+// it has not been set, or where a lane's sum of probabilities passes kFar; no
+// maximum is taken otherwise.  Rows do not touch each other's bits.
+constexpr float kFar = 1024.f;
+__device__ __forceinline__ bool far(float sum, float m) { return !(sum <= kFar) || m == kNegInf; }
+template <typename T, int NKB, int QB>
+__device__ __forceinline__ bool probabilities(const f32x4 (&s)[NKB][QB], const float (&m)[QB], float c,
+                                              u32x4 (&p)[NKB / Mma<T>::kTiles][QB], float (&sum)[QB]) {
+  using M = Mma<T>;
+  bool any = false;
 #pragma unroll
   for (int q = 0; q < QB; ++q) {
-    float m = s[0][q][0];
+    // nothing seen so far: exp2 of -inf - 0 is 0
+    const float base = (m[q] == kNegInf ? 0.f : m[q]) * c;
+    sum[q] = 0.f;
 #pragma unroll
-    for (int k = 0; k < NKB; ++k)
+    for (int t = 0; t < NKB / M::kTiles; ++t) {
+      f32x4 x[M::kTiles];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) m = fmaxf(m, s[k][q][i]);
-    mx[q] = m;
-    moved |= m > st.m[q] + lag;
+      for (int u = 0; u < M::kTiles; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t * M::kTiles + u][q][i], c, -base));
+          sum[q] += x[u][i];
+        }
+      p[t][q] = M::probs(x);
+    }
+    any |= far(sum[q], m[q]);
   }
-  if (__any(moved)) {
+  return any;
+}
+template <typename T, int NKB, int DT16, int QB>
+__device__ __forceinline__ void softmax_step(const f32x4 (&s)[NKB][QB], RowState<DT16, QB>& st, float c,
+                                             u32x4 (&p)[NKB / Mma<T>::kTiles][QB]) {
+  float sum[QB];
+  if (__any(probabilities<T>(s, st.m, c, p, sum))) {
 #pragma unroll
     for (int q = 0; q < QB; ++q) {
-      float m = fmaxf(mx[q], __shfl_xor(mx[q], 16, kWave));
+      int move = far(sum[q], st.m[q]);
+      move |= __shfl_xor(move, 16, kWave);
+      move |= __shfl_xor(move, 32, kWave);
+      float m = s[0][q][0];
+#pragma unroll
+      for (int k = 0; k < NKB; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, s[k][q][i]);
+      m = fmaxf(m, __shfl_xor(m, 16, kWave));
       m = fmaxf(m, __shfl_xor(m, 32, kWave));
-      m = fmaxf(m, st.m[q]);
-      // nothing seen so far: exp2 of -inf - 0 is 0
+      m = move ? fmaxf(m, st.m[q]) : st.m[q];
       const float fade = __builtin_amdgcn_exp2f((st.m[q] - (m == kNegInf ? 0.f : m)) * c);
       st.m[q] = m;
       st.l[q] *= fade;
 #pragma unroll
       for (int d = 0; d < DT16; ++d) st.o[d][q] *= fade;
     }
+    probabilities<T>(s, st.m, c, p, sum);
   }
 #pragma unroll
-  for (int q = 0; q < QB; ++q) {
-    const float base = (st.m[q] == kNegInf ? 0.f : st.m[q]) * c;
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < NKB; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[k][q][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][q][i], c, -base));
-        sum += s[k][q][i];
-      }
-    st.l[q] += sum;
-  }
+  for (int q = 0; q < QB; ++q) st.l[q] += sum[q];
 }
 
-// O^T += V^T P^T over a tile of NKB * 16 keys in LDS.  MASKED: some rows do not
+// O^T += V^T P^T over NS steps of keys in LDS.  MASKED: some rows do not
 // see some of its keys, and 0 times an infinity or a NaN there would reach
 // them; what is not finite is left out (`odd` says so) for add_not_finite().
-template <typename T, int RB, bool MASKED, int NKB, int DT16, int QB>
-__device__ __forceinline__ void weigh(const char* vlds, const uint32_t* vb, const f32x4 (&s)[NKB][QB],
+template <typename T, int RB, bool MASKED, int NS, int DT16, int QB>
+__device__ __forceinline__ void weigh(const char* vlds, const uint32_t* vb, const u32x4 (&p)[NS][QB],
                                       RowState<DT16, QB>& st, uint32_t& odd) {
   using M = Mma<T>;
 #pragma unroll
-  for (int t = 0; t < NKB / M::kTiles; ++t) {
-    u32x4 p[QB];
-#pragma unroll
-    for (int q = 0; q < QB; ++q) {
-      f32x4 x[M::kTiles];
-#pragma unroll
-      for (int u = 0; u < M::kTiles; ++u) x[u] = s[t * M::kTiles + u][q];
-      p[q] = M::probs(x);
-    }
+  for (int t = 0; t < NS; ++t) {
 #pragma unroll
     for (int d = 0; d < DT16; ++d) {
       u32x4 v = M::template vfrag<RB>(vlds, vb, t, d);
@@ -194,7 +201,7 @@ __device__ __forceinline__ void weigh(const char* vlds, const uint32_t* vb, cons
         v = f;
       }
 #pragma unroll
-      for (int q = 0; q < QB; ++q) st.o[d][q] = M::mma(v, p[q], st.o[d][q]);
+      for (int q = 0; q < QB; ++q) st.o[d][q] = M::mma(v, p[t][q], st.o[d][q]);
     }
   }
 }

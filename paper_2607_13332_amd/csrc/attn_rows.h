@@ -8,21 +8,23 @@
 
 namespace ssn {
 
-// Blocks of a compute unit: two where 256 registers hold a wave's rows, keys
-// and values.
 template <typename T, int DT, int QB>
-constexpr int rows_blocks() { return DT * (int)sizeof(T) * QB <= 256 ? 2 : 1; }
+constexpr int rows_join() { return DT / 16 * QB * kWave * 16; }      // bytes of a wave's O
+template <typename T, int DT, int QB>
+constexpr int rows_lds() {
+  const int tiles = 4 * Mma<T>::kKeys * DT * (int)sizeof(T), join = 2 * rows_join<T, DT, QB>();
+  return (tiles > join ? tiles : join) + 4 * QB * kWave * 4;         // and m, l of two waves
+}
 
 template <typename T, int DT, int QB, bool EXACT>
-__global__ __launch_bounds__(256, (rows_blocks<T, DT, QB>())) void paged_attn_rows(AttnArgs a, AttnPart part, int few) {
+__device__ __forceinline__ void rows_block(const AttnArgs& a, const AttnPart& part, int few, int id, char* lds) {
   using M = Mma<T>;
   constexpr int RB = DT * (int)sizeof(T), TK = M::kKeys, NKB = TK / 16, NC = RB / 64, DT16 = DT / 16;
   constexpr int CH = RB / 16, RPI = kWave / CH, NI = TK / RPI;
-  constexpr int kTile = TK * RB, kJoin = DT16 * QB * kWave * 16;    // bytes of a wave
-  __shared__ __align__(16) char lds[4 * kTile > 2 * kJoin ? 4 * kTile : 2 * kJoin];
-  __shared__ float joint[2][2][QB][kWave];
+  constexpr int kTile = TK * RB, kJoin = rows_join<T, DT, QB>();
+  float(*joint)[2][QB][kWave] = (float(*)[2][QB][kWave])(lds + rows_lds<T, DT, QB>() - 4 * QB * kWave * 4);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kh = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk, b = rest % a.pb.B, range = rest / a.pb.B;
+  const int kh = id % a.Hk, rest = id / a.Hk, b = rest % a.pb.B, range = rest / a.pb.B;
   const Sequence sq = sequence_of(a.pb, b);
   const int n = sq.s1 - sq.s0, rows = n * a.G, keys = sq.len;
   if (rows == 0 || rows > few) return;
@@ -42,7 +44,7 @@ __global__ __launch_bounds__(256, (rows_blocks<T, DT, QB>())) void paged_attn_ro
     load_query<NC, EXACT>((const char*)a.Q + ((sq.s0 + token) * a.ldq + (int64_t)(kh * a.G + r % a.G) * a.D) * (int)sizeof(T),
                           bytes, lane, sign_bits<T>(a.scale), a.scale == 0.f, qf[q]);
   }
-  const float c = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * kLog2e, lag = kLag / c;
+  const float c = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * kLog2e;
 
   // A tile's keys go straight to registers as A operands (16 rows x 64 bytes
   // an instruction); its values whole rows at a time, through the wave's part
@@ -109,6 +111,7 @@ __global__ __launch_bounds__(256, (rows_blocks<T, DT, QB>())) void paged_attn_ro
       fetch(next);
       if (t + 8 * TK < k_end) next = key_slot(t + 8 * TK);
     }
+    u32x4 p[NKB / M::kTiles][QB];
     if (masked) {
 #pragma unroll
       for (int q = 0; q < QB; ++q)
@@ -117,11 +120,11 @@ __global__ __launch_bounds__(256, (rows_blocks<T, DT, QB>())) void paged_attn_ro
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (16 * k + 4 * (lane >> 4) + i > seen[q] - t) s[k][q][i] = kNegInf;
-      softmax_step<NKB, DT16, QB>(s, rs, c, lag);
-      weigh<T, RB, true, NKB, DT16, QB>(vl, vb, s, rs, odd);
+      softmax_step<T>(s, rs, c, p);
+      weigh<T, RB, true>(vl, vb, p, rs, odd);
     } else {
-      softmax_step<NKB, DT16, QB>(s, rs, c, lag);
-      weigh<T, RB, false, NKB, DT16, QB>(vl, vb, s, rs, odd);
+      softmax_step<T>(s, rs, c, p);
+      weigh<T, RB, false>(vl, vb, p, rs, odd);
     }
   }
   if (__any(odd != 0)) {
@@ -169,16 +172,6 @@ __global__ __launch_bounds__(256, (rows_blocks<T, DT, QB>())) void paged_attn_ro
   if (wave == 0)
     finish_rows<T, DT, QB, EXACT>(a, part, rs, row, seen, rows, sq.s0, kh, range,
                                   ((int64_t)b * a.Hk + kh) * (16 * QB), ranges == 1, c, lane);
-}
-
-template <typename T, int DT, int QB>
-static hipError_t launch_rows(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
-  const int64_t grid = (int64_t)a.pb.B * a.Hk * p.rows.ranges;
-  if (a.D == DT)
-    hipLaunchKernelGGL((paged_attn_rows<T, DT, QB, true>), dim3((unsigned)grid), dim3(256), 0, st, a, p.rows, p.few);
-  else
-    hipLaunchKernelGGL((paged_attn_rows<T, DT, QB, false>), dim3((unsigned)grid), dim3(256), 0, st, a, p.rows, p.few);
-  return hipGetLastError();
 }
 
 }  // namespace ssn

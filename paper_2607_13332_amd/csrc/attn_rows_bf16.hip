@@ -1,13 +1,13 @@
 // The paged attention's rows kernel for bf16 storage.
-#include "attn_rows.h"
+#include "attn_kernels.h"
 
 namespace ssn {
 
 hipError_t launch_attn_rows_bf16(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const bool one = p.rows.blocks == 1;
-  if (a.D <= 64) return one ? launch_rows<uint16_t, 64, 1>(a, p, st) : launch_rows<uint16_t, 64, 2>(a, p, st);
-  if (a.D <= 128) return one ? launch_rows<uint16_t, 128, 1>(a, p, st) : launch_rows<uint16_t, 128, 2>(a, p, st);
-  return launch_rows<uint16_t, 256, 1>(a, p, st);
+  if (a.D <= 64) return one ? SSN_ATTN_EXACT(launch_rows, uint16_t, 64, 1) : SSN_ATTN_EXACT(launch_rows, uint16_t, 64, 2);
+  if (a.D <= 128) return one ? SSN_ATTN_EXACT(launch_rows, uint16_t, 128, 1) : SSN_ATTN_EXACT(launch_rows, uint16_t, 128, 2);
+  return SSN_ATTN_EXACT(launch_rows, uint16_t, 256, 1);
 }
 
 }  // namespace ssn

@@ -17,6 +17,16 @@ __device__ __forceinline__ int first_tile(const PagedBatch& pb, int b, int G, in
 }
 inline int64_t tile_slots(int64_t N, int64_t B, int64_t G, int64_t BM) { return N * G / BM + B; }
 
+// A sequence's last tiles see the most keys, so they go first; and a compute
+// unit, which gets one block of the first round and one of the second, gets a
+// long and a short one.
+constexpr int kUnits = 256;
+__device__ __forceinline__ int balanced_order(int i, int slots, int Hk) {
+  const int round = kUnits / Hk;
+  if (i < round || i >= 2 * round || slots < 2 * round) return i;
+  return 3 * round - 1 - i;
+}
+
 // What a wave does with its rows when its keys are done: the result, or its
 // part of it.  Row r of the sequence's rows is token r / G, head r % G.
 template <typename T, int DT, int QB, bool EXACT>
@@ -74,16 +84,23 @@ __device__ __forceinline__ uint32_t sign_bits(float scale) {
   return scale < 0.f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
 }
 
+template <typename T, int DT>
+constexpr int tile_keys() { return DT * (int)sizeof(T) <= 256 ? 64 : 32; }
+template <typename T, int DT>
+constexpr int tiles_lds() { return 4 * tile_keys<T, DT>() * DT * (int)sizeof(T); }
+
 template <typename T, int DT, int QB, bool EXACT>
-__global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void paged_attn_tiles(AttnArgs a, AttnPart part, int few, int slots) {
+__device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& part, int few, int slots, int id,
+                                            char* mem) {
   using M = Mma<T>;
-  constexpr int RB = DT * (int)sizeof(T), TK = RB <= 256 ? 64 : 32, NKB = TK / 16, NC = RB / 64;
+  constexpr int RB = DT * (int)sizeof(T), TK = tile_keys<T, DT>(), NC = RB / 64;
+  // keys whose scores are held at a time
+  constexpr int SK = 32, NKB = SK / 16;
   constexpr int CH = RB / 16, RPI = kWave / CH, NI = TK / RPI / 4, BM = 64 * QB;
-  __shared__ __align__(1024) char lds[2][2][TK * RB];     // [buffer][K, V]
+  char(*lds)[2][TK * RB] = (char(*)[2][TK * RB])mem;      // [buffer][K, V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kh = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
-  // a sequence's last tiles see the most keys: they go first
-  const int slot = slots - 1 - rest % slots, range = rest / slots;
+  const int kh = id % a.Hk, rest = id / a.Hk;
+  const int slot = slots - 1 - balanced_order(rest % slots, slots, a.Hk), range = rest / slots;
   const int b = last_at_most(a.pb.B, slot, [&](int i) { return first_tile(a.pb, i, a.G, BM); });
   const Sequence sq = sequence_of(a.pb, b);
   const int n = sq.s1 - sq.s0, rows = n * a.G, tile = slot - first_tile(a.pb, b, a.G, BM);
@@ -107,7 +124,7 @@ __global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void pag
                           bytes, lane, sign_bits<T>(a.scale), a.scale == 0.f, qf[q]);
   }
   // a scale of zero: zero queries, any other scale
-  const float c = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * kLog2e, lag = kLag / c;
+  const float c = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * kLog2e;
   const int wave_last = r0 + (wave + 1) * (16 * QB) - 1;
   const int seen_hi = before + (wave_last < rows ? wave_last : rows - 1) / a.G;
 
@@ -136,7 +153,7 @@ __global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void pag
   };
   if constexpr (!EXACT) {
     // chunks past a row's end are never loaded: zero once
-    for (int i = threadIdx.x * 16; i < (int)sizeof(lds); i += 256 * 16) *(u32x4*)(&lds[0][0][0] + i) = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x * 16; i < tiles_lds<T, DT>(); i += 256 * 16) *(u32x4*)(mem + i) = u32x4{0, 0, 0, 0};
     __syncthreads();
   }
 
@@ -161,6 +178,10 @@ __global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void pag
     if (t + 1 < t1) fetch(next, (t + 1 - t0) & 1);
     if (t + 2 < t1) next = key_slot(t + 2);
   };
+  // The widest tiles ask for the matrix cores first (s_setprio), so that of a
+  // SIMD's two waves one multiplies while the other exponentiates: 4 % at 192
+  // rows (8192-token prompt 698 -> 679 us), nothing below.
+  constexpr bool kFirst = QB == 3;
   auto scores = [&](const char* kl, f32x4 (&s)[NKB][QB]) {
 #pragma unroll
     for (int k = 0; k < NKB; ++k) {
@@ -180,27 +201,40 @@ __global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void pag
   int t = t0;
   for (; t < t_open; ++t) {
     arrive(t);
-    const int buf = (t - t0) & 1;
-    f32x4 s[NKB][QB];
-    scores(lds[buf][0], s);
-    softmax_step<NKB, DT / 16, QB>(s, rs, c, lag);
-    weigh<T, RB, false, NKB, DT / 16, QB>(lds[buf][1], vb, s, rs, odd);
+    const char *kl = lds[(t - t0) & 1][0], *vl = lds[(t - t0) & 1][1];
+#pragma unroll
+    for (int u = 0; u < TK; u += SK) {
+      f32x4 s[NKB][QB];
+      if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
+      scores(kl + u * RB, s);
+      if constexpr (kFirst) __builtin_amdgcn_s_setprio(0);
+      u32x4 p[NKB / M::kTiles][QB];
+      softmax_step<T>(s, rs, c, p);
+      if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
+      weigh<T, RB, false>(vl + u * RB, vb, p, rs, odd);
+      if constexpr (kFirst) __builtin_amdgcn_s_setprio(0);
+    }
   }
   for (; t < t1; ++t) {
     arrive(t);
-    const int buf = (t - t0) & 1, k0 = t * TK;
-    if (k0 > seen_hi) continue;
-    f32x4 s[NKB][QB];
-    scores(lds[buf][0], s);
+    const char *kl = lds[(t - t0) & 1][0], *vl = lds[(t - t0) & 1][1];
+#pragma unroll 1
+    for (int u = 0; u < TK; u += SK) {
+      const int k0 = t * TK + u;
+      if (k0 > seen_hi) break;
+      f32x4 s[NKB][QB];
+      scores(kl + u * RB, s);
 #pragma unroll
-    for (int q = 0; q < QB; ++q)
+      for (int q = 0; q < QB; ++q)
 #pragma unroll
-      for (int k = 0; k < NKB; ++k)
+        for (int k = 0; k < NKB; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (16 * k + 4 * (lane >> 4) + i > seen[q] - k0) s[k][q][i] = kNegInf;
-    softmax_step<NKB, DT / 16, QB>(s, rs, c, lag);
-    weigh<T, RB, true, NKB, DT / 16, QB>(lds[buf][1], vb, s, rs, odd);
+          for (int i = 0; i < 4; ++i)
+            if (16 * k + 4 * (lane >> 4) + i > seen[q] - k0) s[k][q][i] = kNegInf;
+      u32x4 p[NKB / M::kTiles][QB];
+      softmax_step<T>(s, rs, c, p);
+      weigh<T, RB, true>(vl + u * RB, vb, p, rs, odd);
+    }
   }
   if (__any(odd != 0)) {
     // the keys of the masked tiles
@@ -213,18 +247,6 @@ __global__ __launch_bounds__(256, (DT * (int)sizeof(T) <= 512 ? 2 : 1)) void pag
     }
   }
   finish_rows<T, DT, QB, EXACT>(a, part, rs, row, seen, rows, sq.s0, kh, range, -1, ranges == 1, c, lane);
-}
-
-template <typename T, int DT, int QB>
-static hipError_t launch_tiles(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
-  const int64_t slots = tile_slots(a.pb.N, a.pb.B, a.G, 64 * QB), grid = slots * a.Hk * p.tiles.ranges;
-  if (a.D == DT)
-    hipLaunchKernelGGL((paged_attn_tiles<T, DT, QB, true>), dim3((unsigned)grid), dim3(256), 0, st, a, p.tiles,
-                       p.few, (int)slots);
-  else
-    hipLaunchKernelGGL((paged_attn_tiles<T, DT, QB, false>), dim3((unsigned)grid), dim3(256), 0, st, a, p.tiles,
-                       p.few, (int)slots);
-  return hipGetLastError();
 }
 
 }  // namespace ssn

@@ -1,13 +1,13 @@
-// The paged attention's tile kernel for f32 storage.
-#include "attn_tiles.h"
+// The paged attention's tile kernel (and with it the rows kernel, where a batch
+// has both) for f32 storage.
+#include "attn_kernels.h"
 
 namespace ssn {
 
 hipError_t launch_attn_tiles_f32(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
-  const bool one = p.tiles.blocks == 1;
-  if (a.D <= 64) return one ? launch_tiles<float, 64, 1>(a, p, st) : launch_tiles<float, 64, 2>(a, p, st);
-  if (a.D <= 128) return one ? launch_tiles<float, 128, 1>(a, p, st) : launch_tiles<float, 128, 2>(a, p, st);
-  return launch_tiles<float, 256, 1>(a, p, st);
+  if (a.D <= 64) return SSN_ATTN_EXACT(launch_tiles, float, 64, 1);
+  if (a.D <= 128) return SSN_ATTN_EXACT(launch_tiles, float, 128, 1);
+  return SSN_ATTN_EXACT(launch_tiles, float, 256, 1);
 }
 
 }  // namespace ssn

@@ -71,10 +71,11 @@ __global__ __launch_bounds__(256) void paged_attn_generic(AttnArgs a) {
 }
 
 // Joins the partial results of a row's ranges: with M the largest m, O = sum
-// exp2(m - M) O_r / sum exp2(m - M) l_r, in a fixed order.  A wave owns a row:
-// lane i the (m, l) of ranges i, i + 64, ..; then `lanes` lanes the row's
-// elements, four each, the groups of them the ranges in turn.
-constexpr int kMaxRanges = 256, kRangeChunks = kMaxRanges / kWave;
+// exp2(m - M) O_r / sum exp2(m - M) l_r, in a fixed order.  `lanes` lanes of a
+// wave own a row, four elements each; with up to `lanes` ranges every group of
+// them takes a row of its own (of one token), with more the groups share one
+// and take the ranges in turn.
+constexpr int kMaxRanges = 256;
 
 // Row r of sequence b and key head kh, its partial results at `at`.
 struct JoinRow {
@@ -82,21 +83,8 @@ struct JoinRow {
   int64_t at;
   Sequence sq;
 };
-// Line `line` of the rows kernel's stage, or of the batch's (token, head) pairs.
 template <bool FEW>
-__device__ __forceinline__ bool join_row(const AttnArgs& a, const AttnPart& p, int few, int line, JoinRow& j) {
-  if constexpr (FEW) {
-    const int per = 16 * p.blocks;
-    j.r = line % per;
-    j.kh = line / per % a.Hk;
-    j.b = line / per / a.Hk;
-  } else {
-    const int token = line / a.Hq, head = line - token * a.Hq;
-    j.b = sequence_of_row(a.pb, token);
-    if (j.b < 0) return false;
-    j.kh = head / a.G;
-    j.r = (token - clampi(a.pb.starts[j.b], 0, a.pb.N)) * a.G + head % a.G;
-  }
+__device__ __forceinline__ bool join_row(const AttnArgs& a, const AttnPart& p, int few, JoinRow& j) {
   j.sq = sequence_of(a.pb, j.b);
   const int n = j.sq.s1 - j.sq.s0, rows = n * a.G;
   if (j.r >= rows || (rows <= few) != FEW) return false;
@@ -105,70 +93,111 @@ __device__ __forceinline__ bool join_row(const AttnArgs& a, const AttnPart& p, i
     const int bm = 64 * p.blocks, last = (j.r / bm + 1) * bm - 1;
     keys = j.sq.len - n + (last < rows ? last : rows - 1) / a.G + 1;
   }
-  j.at = line;
   j.ranges = keys > p.chunk ? (keys + p.chunk - 1) / p.chunk : 1;
   return j.ranges > 1;
 }
 
-template <typename T, bool FEW>
-__global__ __launch_bounds__(256) void paged_attn_join(AttnArgs a, AttnPart p, int few, int lines, int lanes) {
-  const int lane = threadIdx.x & 63;
-  for (int line = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6))); line < lines;
-       line += gridDim.x * 4) {
+// One wave: `share` lanes to a row.
+template <typename T>
+__device__ __forceinline__ void join_line(const AttnArgs& a, const AttnPart& p, const JoinRow& j, bool mine,
+                                          int lanes, int share) {
+  const int lane = threadIdx.x & 63, at = lane & (share - 1);
+  float top = kNegInf;
+  for (int g = at; g < j.ranges; g += share) top = fmaxf(top, p.ml[2 * (g * p.stage_rows + j.at)]);
+  for (int m = share / 2; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, kWave));
+  const float base = top == kNegInf ? 0.f : top;
+  const int e = (lane & (lanes - 1)) * 4, groups = share / lanes;
+  float sum = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int g0 = at / lanes; g0 < j.ranges; g0 += 8 * groups) {
+    f32x4 x[8];
+    f32x2 ml[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {          // eight ranges in flight
+      const int g = g0 + u * groups;
+      x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      ml[u] = f32x2{kNegInf, 0.f};
+      if (g < j.ranges) {
+        ml[u] = *(const f32x2*)(p.ml + 2 * (g * p.stage_rows + j.at));
+        if (e < a.D) x[u] = *(const f32x4*)(p.o + (g * p.stage_rows + j.at) * a.D + e);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float w = __builtin_amdgcn_exp2f(ml[u][0] - base);
+      sum += ml[u][1] * w;
+      o += x[u] * w;
+    }
+  }
+  for (int m = lanes; m < share; m <<= 1) {
+    sum += __shfl_xor(sum, m, kWave);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m, kWave);
+  }
+  const int64_t token = j.sq.s0 + j.r / a.G;
+  const int head = j.kh * a.G + j.r % a.G;
+  const bool sees = j.sq.len - (j.sq.s1 - (int)token) >= 0;
+  if (mine && at < lanes && e < a.D)
+    store4((T*)a.O + token * a.ldo + (int64_t)head * a.D + e, o * (sees ? 1.f / sum : 0.f));
+  if (mine && a.lse && at == 0)
+    a.lse[token * a.Hq + head] = sees ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f : kNegInf;
+}
+
+// Units of the tiles' lines (a token and `pt` of its heads), then of the rows
+// kernel's (a sequence, a key head and `pr` of its rows): one wave each, pt and
+// pr 1 or 64 / lanes.
+struct JoinShape {
+  int lanes, pt, pr, tile_units, units;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void paged_attn_join(AttnArgs a, AttnPlan plan, JoinShape js) {
+  const int lane = threadIdx.x & 63, sub = lane / js.lanes;
+  for (int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6))); unit < js.units;
+       unit += gridDim.x * 4) {
     JoinRow j;
-    if (!join_row<FEW>(a, p, few, line, j)) continue;
-    float w[kRangeChunks], sum = 0.f, top = kNegInf;
-#pragma unroll
-    for (int c = 0; c < kRangeChunks; ++c) {
-      w[c] = kNegInf;
-      if (c * kWave + lane < j.ranges) w[c] = p.ml[2 * ((c * kWave + lane) * p.stage_rows + j.at)];
-      top = fmaxf(top, w[c]);
+    if (unit < js.tile_units) {
+      const int per = (a.Hq + js.pt - 1) / js.pt, token = unit / per, h0 = (unit - token * per) * js.pt;
+      j.b = sequence_of_row(a.pb, token);
+      if (j.b < 0) continue;
+      const bool mine = js.pt == 1 || h0 + sub < a.Hq;
+      const int head = js.pt == 1 ? h0 : (mine ? h0 + sub : h0);
+      j.kh = head / a.G;
+      j.r = (token - clampi(a.pb.starts[j.b], 0, a.pb.N)) * a.G + head % a.G;
+      j.at = (int64_t)token * a.Hq + head;
+      // (lanes of different rows may differ in the ranges of their tiles)
+      if (join_row<false>(a, plan.tiles, plan.few, j))
+        join_line<T>(a, plan.tiles, j, mine, js.lanes, js.pt == 1 ? kWave : js.lanes);
+    } else {
+      const int rows = 16 * plan.rows.blocks, per = rows / js.pr, i = unit - js.tile_units;
+      const int r0 = i % per * js.pr;
+      j.kh = i / per % a.Hk;
+      j.b = i / per / a.Hk;
+      j.r = r0 + (js.pr == 1 ? 0 : sub);
+      j.at = ((int64_t)j.b * a.Hk + j.kh) * rows + j.r;
+      if (join_row<true>(a, plan.rows, plan.few, j))
+        join_line<T>(a, plan.rows, j, true, js.lanes, js.pr == 1 ? kWave : js.lanes);
     }
-    top = wave_max(top);
-#pragma unroll
-    for (int c = 0; c < kRangeChunks; ++c)
-      if (c * kWave + lane < j.ranges) {
-        w[c] = __builtin_amdgcn_exp2f(w[c] - (top == kNegInf ? 0.f : top));
-        sum += p.ml[2 * ((c * kWave + lane) * p.stage_rows + j.at) + 1] * w[c];
-      }
-    sum = wave_sum(sum);
-    const int e = (lane & (lanes - 1)) * 4, groups = kWave / lanes;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < kRangeChunks; ++c) {
-      const int n = j.ranges - c * kWave < kWave ? j.ranges - c * kWave : kWave;
-#pragma unroll 4
-      for (int g = 0; g < n; g += groups) {
-        const int mine = g + lane / lanes;
-        const float weight = __shfl(w[c], mine & 63, kWave);
-        if (mine < n && e < a.D)
-          o += *(const f32x4*)(p.o + ((c * kWave + mine) * p.stage_rows + j.at) * a.D + e) * weight;
-      }
-    }
-    for (int m = lanes; m < kWave; m <<= 1)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m, kWave);
-    const int64_t token = j.sq.s0 + j.r / a.G;
-    const int head = j.kh * a.G + j.r % a.G;
-    const bool sees = j.sq.len - (j.sq.s1 - (int)token) >= 0;
-    if (lane < lanes && e < a.D)
-      store4((T*)a.O + token * a.ldo + (int64_t)head * a.D + e, o * (sees ? 1.f / sum : 0.f));
-    if (a.lse && lane == 0)
-      a.lse[token * a.Hq + head] = sees ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f : kNegInf;
   }
 }
 
-template <bool FEW>
-static hipError_t launch_join(int dtype, const AttnArgs& a, const AttnPart& p, int few, hipStream_t st) {
-  if (p.blocks == 0 || p.ranges <= 1) return hipSuccess;
-  int lanes = 1;
-  while (lanes * 4 < a.D) lanes *= 2;
-  const int lines = (int)p.stage_rows;
-  const dim3 grid((unsigned)((lines + 3) / 4 < (1 << 20) ? (lines + 3) / 4 : (1 << 20)));
+static hipError_t launch_join(int dtype, const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
+  JoinShape js;
+  js.lanes = 1;
+  while (js.lanes * 4 < a.D) js.lanes *= 2;
+  js.pt = p.tiles.ranges <= js.lanes ? kWave / js.lanes : 1;
+  js.pr = p.rows.ranges <= js.lanes ? kWave / js.lanes : 1;
+  if (js.pr > 16) js.pr = 16;
+  const int64_t tiles = p.tiles.blocks && p.tiles.ranges > 1 ? a.pb.N * (int64_t)((a.Hq + js.pt - 1) / js.pt) : 0;
+  const int64_t rows = p.rows.blocks && p.rows.ranges > 1 ? p.rows.stage_rows / js.pr : 0;
+  if (tiles + rows == 0) return hipSuccess;
+  js.tile_units = (int)tiles;
+  js.units = (int)(tiles + rows);
+  const int64_t blocks = (tiles + rows + 3) / 4;
+  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
   if (dtype == kBF16)
-    hipLaunchKernelGGL((paged_attn_join<uint16_t, FEW>), grid, dim3(256), 0, st, a, p, few, lines, lanes);
+    hipLaunchKernelGGL((paged_attn_join<uint16_t>), grid, dim3(256), 0, st, a, p, js);
   else
-    hipLaunchKernelGGL((paged_attn_join<float, FEW>), grid, dim3(256), 0, st, a, p, few, lines, lanes);
+    hipLaunchKernelGGL((paged_attn_join<float>), grid, dim3(256), 0, st, a, p, js);
   return hipGetLastError();
 }
 
@@ -187,25 +216,38 @@ static void split_keys(AttnPart& p, int64_t want, int64_t unit, int64_t max_len,
   p.chunk = (int)chunk;
   p.ranges = (int)((len + p.chunk - 1) / p.chunk);
 }
-static AttnPlan attention_plan(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
+// 16-row blocks of a tile kernel's wave, 1 to 3.  More rows make more of every
+// key read from LDS, fewer make more blocks: tiles of 192 rows where they fill
+// the chip one and a half times, of 128 where they fill three quarters of it
+// (the two blocks of a compute unit counted), else of 64.  bf16, 40 / 8 heads of
+// 128, one prompt, us for 64 / 128 / 192 rows: 1024 tokens 29 / 33 / 63, 2048
+// 81 / 63 / 80, 4096 277 / 202 / 192.  Over long caches keys are split to fill
+// the chip instead: 512 tokens over 32768 keys 583 / 356 / 314.  With heads of
+// 64, 192 rows gain nothing; float32 takes 64 (2048 tokens of 16 heads of 64: 687
+// us, 698 with 128 rows; 1024 tokens 80, 127).
+static int tile_rows(int dtype, int64_t rows, int64_t most, int64_t Hk, int64_t D, int64_t max_len) {
+  if (dtype != kBF16 || D > 128 || most <= 64) return 1;
+  const bool split = max_len >= 8192;
+  if (D > 64 && (split || rows * Hk / 192 >= 768)) return 3;
+  return split || rows * Hk / 128 >= 384 ? 2 : 1;
+}
+static AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
                                int64_t max_len, size_t ws_bytes) {
   AttnPlan p = {};
   const int64_t G = Hq / Hk, most = max_q * G;
-  const bool wide = D > 128;
-  if (most <= 16 || (most <= 32 && !wide)) {
-    p.few = most <= 16 ? 16 : 32;
-  } else {
-    // single tokens among longer chunks, unless all have max_q
-    if (G <= 16 && N != B * max_q) p.few = 16;
-    p.tiles.blocks = (most <= 64 || wide) ? 1 : 2;
-  }
+  const bool tiles = most > 32 || (most > 16 && D > 128);
+  // the rows kernel takes all sequences, or the single tokens among longer
+  // chunks (unless all have max_q)
+  if (!tiles) p.few = most <= 16 ? 16 : 32;
+  else if (G <= 16 && N != B * max_q) p.few = 16;
   p.rows.blocks = (p.few + 15) / 16;
   p.rows.stage_rows = B * Hk * 16 * p.rows.blocks;
   p.tiles.stage_rows = N * Hq;
-  if (p.tiles.blocks) {
+  if (tiles) {
+    const int64_t rows = (p.few && N - B >= 0 ? N - B + 1 : N) * G;
+    p.tiles.blocks = tile_rows(dtype, rows, most, Hk, D, max_len);
     // two blocks to a compute unit, where the rows alone do not give them
-    const int64_t big = p.few ? (N - B + 1 > 1 ? N - B + 1 : 1) : N;
-    const int64_t blocks = (big * G / (64 * p.tiles.blocks) + 1) * Hk;
+    const int64_t blocks = (rows / (64 * p.tiles.blocks) + 1) * Hk;
     split_keys(p.tiles, blocks >= 512 ? 1 : 512 / blocks, 256, max_len, D, ws_bytes);
   }
   if (p.rows.blocks) {
@@ -216,10 +258,10 @@ static AttnPlan attention_plan(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int
   return p;
 }
 
-size_t attention_workspace_bytes(int, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
+size_t attention_workspace_bytes(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
                                  int64_t max_len) {
   if (D > 256) return 0;
-  const AttnPlan p = attention_plan(N, B, Hq, Hk, D, max_q, max_len, (size_t)1 << 60);
+  const AttnPlan p = attention_plan(dtype, N, B, Hq, Hk, D, max_q, max_len, (size_t)1 << 60);
   return stage_bytes(p.tiles, D) + stage_bytes(p.rows, D);
 }
 
@@ -240,7 +282,7 @@ hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void* ws, size_t
       hipLaunchKernelGGL((paged_attn_generic<float>), dim3(grid), dim3(256), 0, st, a);
     return hipGetLastError();
   }
-  AttnPlan p = attention_plan(a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0);
+  AttnPlan p = attention_plan(dtype, a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0);
   float* at = (float*)ws;
   for (AttnPart* x : {&p.tiles, &p.rows})
     if (stage_bytes(*x, a.D)) {
@@ -248,12 +290,10 @@ hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void* ws, size_t
       x->ml = at + x->ranges * x->stage_rows * a.D;
       at = x->ml + x->ranges * x->stage_rows * 2;
     }
-  hipError_t e = hipSuccess;
+  hipError_t e;
   if (p.tiles.blocks) e = dtype == kBF16 ? launch_attn_tiles_bf16(a, p, st) : launch_attn_tiles_f32(a, p, st);
-  if (e == hipSuccess && p.rows.blocks)
-    e = dtype == kBF16 ? launch_attn_rows_bf16(a, p, st) : launch_attn_rows_f32(a, p, st);
-  if (e == hipSuccess) e = launch_join<false>(dtype, a, p.tiles, p.few, st);
-  return e == hipSuccess ? launch_join<true>(dtype, a, p.rows, p.few, st) : e;
+  else e = dtype == kBF16 ? launch_attn_rows_bf16(a, p, st) : launch_attn_rows_f32(a, p, st);
+  return e == hipSuccess ? launch_join(dtype, a, p, st) : e;
 }
 
 }  // namespace ssn
