@@ -545,7 +545,7 @@ ssn_status_t ssn_qk_norm_rope_backward(ssn_dtype_t dtype, int64_t N, int64_t Hq,
  * (to npages, N, width * page_size and, in the attention, max_len), so memory
  * stays in bounds, and the results are unspecified.  width * page_size,
  * npages * Hk * page_size and N * (Hq + 2 Hk) stay below 2^31 - 4096 and B
- * below 2^20; in the attention N * Hq below 2^29 and B * Hk below 2^22.
+ * below 2^20; in the attention N * Hq below 2^28 and B * Hk below 2^22.
  */
 
 /*

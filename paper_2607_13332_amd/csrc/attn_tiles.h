@@ -10,12 +10,70 @@ namespace ssn {
 typedef __attribute__((address_space(3))) uint32_t lds_word;
 typedef __attribute__((address_space(1))) const uint32_t global_word;
 
-// Tile of rows `tile` of the launch: sequence b has the slots from starts[b] *
-// G / BM + b on, which leaves ceil(rows / BM) to each.
-__device__ __forceinline__ int first_tile(const PagedBatch& pb, int b, int G, int BM) {
+// The launch's row tiles.  Up to kCounted sequences every block counts them
+// (a wave scans the row counts), so that the tiles there are come first in the
+// grid; past that sequence b has the numbers from starts[b] * G / BM + b on,
+// which leaves ceil(rows / BM) to each, and some numbers name none.
+constexpr int kCounted = 256;
+inline int64_t tile_slots(int64_t N, int64_t B, int64_t G, int64_t BM) { return N * G / BM + B; }
+__device__ __forceinline__ int first_slot(const PagedBatch& pb, int b, int G, int BM) {
   return (int)((int64_t)clampi(pb.starts[b], 0, pb.N) * G / BM) + b;
 }
-inline int64_t tile_slots(int64_t N, int64_t B, int64_t G, int64_t BM) { return N * G / BM + B; }
+__device__ __forceinline__ int tiles_of(const PagedBatch& pb, int b, int G, int BM, int few) {
+  if (b >= pb.B) return 0;
+  const int s0 = clampi(pb.starts[b], 0, pb.N), rows = (clampi(pb.starts[b + 1], s0, pb.N) - s0) * G;
+  return rows > few ? (rows + BM - 1) / BM : 0;
+}
+struct TileCount {
+  int mine[kCounted / kWave];     // tiles of sequence 64 c + lane
+  int total;
+  __device__ __forceinline__ void count(const PagedBatch& pb, int G, int BM, int few, int slots) {
+    if (pb.B > kCounted) {
+      total = slots;
+      return;
+    }
+    int n = 0;
+#pragma unroll
+    for (int c = 0; c < kCounted / kWave; ++c) {
+      mine[c] = 64 * c < pb.B ? tiles_of(pb, 64 * c + (threadIdx.x & 63), G, BM, few) : 0;
+      n += mine[c];
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) n += __shfl_xor(n, m, kWave);
+    // contents past the contract may count more than the grid has
+    total = __builtin_amdgcn_readfirstlane(n < slots ? n : slots);
+  }
+  // Sequence and tile of it of number i < total; false: none.
+  __device__ __forceinline__ bool find(const PagedBatch& pb, int G, int BM, int few, int i, int& b, int& tile) const {
+    if (pb.B > kCounted) {
+      b = last_at_most(pb.B, i, [&](int x) { return first_slot(pb, x, G, BM); });
+      tile = i - first_slot(pb, b, G, BM);
+      return tile >= 0 && tile < tiles_of(pb, b, G, BM, few);
+    }
+    int before = 0;
+    const int lane = threadIdx.x & 63;
+    for (int c = 0; c < kCounted / kWave; ++c) {
+      int sum = c == 0 ? mine[0] : (c == 1 ? mine[1] : (c == 2 ? mine[2] : mine[3]));
+      const int own = sum;
+#pragma unroll
+      for (int m = 1; m < kWave; m <<= 1) {
+        const int x = __shfl_up(sum, m, kWave);
+        if (lane >= m) sum += x;
+      }
+      const uint64_t hit = __ballot(before + sum > i);
+      if (hit) {
+        const int l = __ffsll((unsigned long long)hit) - 1;
+        b = 64 * c + l;
+        tile = i - before - (__shfl(sum, l, kWave) - __shfl(own, l, kWave));
+        b = __builtin_amdgcn_readfirstlane(b);
+        tile = __builtin_amdgcn_readfirstlane(tile);
+        return true;
+      }
+      before += __shfl(sum, 63, kWave);
+    }
+    return false;
+  }
+};
 
 // A sequence's last tiles see the most keys, so they go first; and a compute
 // unit, which gets one block of the first round and one of the second, gets a
@@ -90,8 +148,8 @@ template <typename T, int DT>
 constexpr int tiles_lds() { return 4 * tile_keys<T, DT>() * DT * (int)sizeof(T); }
 
 template <typename T, int DT, int QB, bool EXACT>
-__device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& part, int few, int slots, int id,
-                                            char* mem) {
+__device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& part, int few, const TileCount& count,
+                                            int id, char* mem) {
   using M = Mma<T>;
   constexpr int RB = DT * (int)sizeof(T), TK = tile_keys<T, DT>(), NC = RB / 64;
   // keys whose scores are held at a time
@@ -100,12 +158,14 @@ __device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& p
   char(*lds)[2][TK * RB] = (char(*)[2][TK * RB])mem;      // [buffer][K, V]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kh = id % a.Hk, rest = id / a.Hk;
-  const int slot = slots - 1 - balanced_order(rest % slots, slots, a.Hk), range = rest / slots;
-  const int b = last_at_most(a.pb.B, slot, [&](int i) { return first_tile(a.pb, i, a.G, BM); });
+  if (count.total <= 0) return;
+  const int range = rest / count.total;
+  int b, tile;
+  if (range >= part.ranges ||
+      !count.find(a.pb, a.G, BM, few, count.total - 1 - balanced_order(rest % count.total, count.total, a.Hk), b, tile))
+    return;
   const Sequence sq = sequence_of(a.pb, b);
-  const int n = sq.s1 - sq.s0, rows = n * a.G, tile = slot - first_tile(a.pb, b, a.G, BM);
-  if (tile < 0 || (int64_t)tile * BM >= rows || rows <= few) return;
-  const int r0 = tile * BM;
+  const int n = sq.s1 - sq.s0, rows = n * a.G, r0 = tile * BM;
   const int before = sq.len - n;                           // position of the sequence's token 0
   const int last = r0 + BM < rows ? r0 + BM - 1 : rows - 1;
   const int keys = before + last / a.G + 1;                // that the tile sees

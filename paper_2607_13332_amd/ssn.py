@@ -647,7 +647,7 @@ def delta_rule(theta: torch.Tensor, avg: torch.Tensor, snap: Optional[torch.Tens
 ROPE_STYLES = {"halves": 0, "pairs": 1}
 
 
-def _rows(t: torch.Tensor, name: str, first: torch.Tensor, dev: int, dtype, shape) -> tuple:
+def _rows(t: torch.Tensor, name: str, first: torch.Tensor, dev: int, dtype, N: int, H: int, D: int) -> tuple:
     """(data_ptr, row stride) of a tensor [N, H, D] on the GPU `dev` of the
     call's `first` tensor, heads of a row packed."""
     if t.get_device() != dev or t.dtype != dtype or dev < 0:
@@ -655,13 +655,14 @@ def _rows(t: torch.Tensor, name: str, first: torch.Tensor, dev: int, dtype, shap
         if dev < 0 or not t.is_cuda:
             raise ValueError(f"{name} must be a GPU tensor (the codec has no CPU path)")
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    N, H, D = shape
+    if t.shape != (N, H, D):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(N, H, D)}")
     ld, sh, se = t.stride()
-    if (se != 1 and D > 1) or (sh != D and H > 1) or (ld < H * D and N > 1):
+    if N <= 1:
+        ld = H * D
+    if (se != 1 and D > 1) or (sh != D and H > 1) or ld < H * D:
         raise ValueError(f"the heads of a row of {name} must be contiguous, got strides {t.stride()}")
-    return t.data_ptr(), (ld if N > 1 else H * D)
+    return t.data_ptr(), ld
 
 
 def _rotation(table, style, eps, D, wq, wk):
@@ -677,7 +678,7 @@ def _rotation(table, style, eps, D, wq, wk):
 def _weight(w, name, first, dev, dtype, D):
     if w is None:
         return None
-    if w.shape != (D,):
+    if w.numel() != D:
         raise ValueError(f"{name} has shape {tuple(w.shape)}, expected ({D},)")
     return _gpu(w, name, first, dev, dtype, 1)
 
@@ -714,11 +715,11 @@ def qk_norm_rope(Q: torch.Tensor, K: torch.Tensor, pos: Optional[torch.Tensor] =
     if R and (pos is None or pos.shape != (N,)):
         raise ValueError(f"pos must be [{N}] positions")
     _check("ssn_qk_norm_rope", lib().ssn_qk_norm_rope(
-        _code(t), N, Hq, Hk, D, R, P, code, e, *_rows(Q, "Q", Q, g, t, (N, Hq, D)),
-        *_rows(K, "K", Q, g, t, (N, Hk, D)), _weight(wq, "wq", Q, g, t, D), _weight(wk, "wk", Q, g, t, D),
+        _code(t), N, Hq, Hk, D, R, P, code, e, *_rows(Q, "Q", Q, g, t, N, Hq, D),
+        *_rows(K, "K", Q, g, t, N, Hk, D), _weight(wq, "wq", Q, g, t, D), _weight(wk, "wk", Q, g, t, D),
         _gpu(pos, "pos", Q, g, torch.int32, 1) if R else None,
         _gpu(table, "table", Q, g, torch.float32, 2) if R else None,
-        *_rows(Qout, "Qout", Q, g, t, (N, Hq, D)), *_rows(Kout, "Kout", Q, g, t, (N, Hk, D)),
+        *_rows(Qout, "Qout", Q, g, t, N, Hq, D), *_rows(Kout, "Kout", Q, g, t, N, Hk, D),
         _stream(stream)))
     return Qout, Kout
 
@@ -762,12 +763,12 @@ def qk_norm_rope_backward(Q: torch.Tensor, K: torch.Tensor, GQ: torch.Tensor, GK
     if R and (pos is None or pos.shape != (N,)):
         raise ValueError(f"pos must be [{N}] positions")
     _check("ssn_qk_norm_rope_backward", lib().ssn_qk_norm_rope_backward(
-        _code(t), N, Hq, Hk, D, R, P, code, e, *_rows(Q, "Q", Q, g, t, (N, Hq, D)),
-        *_rows(K, "K", Q, g, t, (N, Hk, D)), _weight(wq, "wq", Q, g, t, D), _weight(wk, "wk", Q, g, t, D),
+        _code(t), N, Hq, Hk, D, R, P, code, e, *_rows(Q, "Q", Q, g, t, N, Hq, D),
+        *_rows(K, "K", Q, g, t, N, Hk, D), _weight(wq, "wq", Q, g, t, D), _weight(wk, "wk", Q, g, t, D),
         _gpu(pos, "pos", Q, g, torch.int32, 1) if R else None,
         _gpu(table, "table", Q, g, torch.float32, 2) if R else None,
-        *_rows(GQ, "GQ", Q, g, t, (N, Hq, D)), *_rows(GK, "GK", Q, g, t, (N, Hk, D)),
-        *_rows(GQin, "GQin", Q, g, t, (N, Hq, D)), *_rows(GKin, "GKin", Q, g, t, (N, Hk, D)),
+        *_rows(GQ, "GQ", Q, g, t, N, Hq, D), *_rows(GK, "GK", Q, g, t, N, Hk, D),
+        *_rows(GQin, "GQin", Q, g, t, N, Hq, D), *_rows(GKin, "GKin", Q, g, t, N, Hk, D),
         _weight(Gwq, "Gwq", Q, g, torch.float32, D), _weight(Gwk, "Gwk", Q, g, torch.float32, D),
         None if workspace is None else _gpu(workspace, "workspace", Q, g, torch.uint8, 1),
         0 if workspace is None else workspace.numel(), _stream(stream)))
@@ -776,18 +777,20 @@ def qk_norm_rope_backward(Q: torch.Tensor, K: torch.Tensor, GQ: torch.Tensor, GK
 
 def _paged(Kc, Vc, pages, starts, lens, first, g, t, Hk, D):
     """(B, C arguments) of a batch of sequences over the paged cache."""
-    if Kc.dim() != 4 or Kc.shape[1] != Hk or Kc.shape[3] != D or Vc.shape != Kc.shape:
-        raise ValueError(f"shape mismatch Kc{tuple(Kc.shape)} Vc{tuple(Vc.shape)}, expected "
+    kc = Kc.shape
+    if len(kc) != 4 or kc[1] != Hk or kc[3] != D or Vc.shape != kc:
+        raise ValueError(f"shape mismatch Kc{tuple(kc)} Vc{tuple(Vc.shape)}, expected "
                          f"(pages, {Hk}, page_size, {D})")
     if pages.dim() != 2:
         raise ValueError(f"pages must be [B, width], got {tuple(pages.shape)}")
     B, width = pages.shape
-    if starts.shape != (B + 1,) or lens.shape != (B,):
+    if starts.numel() != B + 1 or lens.numel() != B:
         raise ValueError(f"shape mismatch pages{tuple(pages.shape)} starts{tuple(starts.shape)} "
                          f"lens{tuple(lens.shape)}")
-    return B, (_gpu(Kc, "Kc", first, g, t, 4), _gpu(Vc, "Vc", first, g, t, 4), Kc.shape[0], Kc.shape[2],
-               _gpu(pages, "pages", first, g, torch.int32, 2), width,
-               _gpu(starts, "starts", first, g, torch.int32, 1), _gpu(lens, "lens", first, g, torch.int32, 1))
+    i32 = torch.int32
+    return B, (_gpu(Kc, "Kc", first, g, t, 4), _gpu(Vc, "Vc", first, g, t, 4), kc[0], kc[2],
+               _gpu(pages, "pages", first, g, i32, 2), width,
+               _gpu(starts, "starts", first, g, i32, 1), _gpu(lens, "lens", first, g, i32, 1))
 
 
 def kv_append(K: torch.Tensor, V: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor,
@@ -808,12 +811,12 @@ def kv_append(K: torch.Tensor, V: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tens
         Hq = Q.shape[1]
         if Qout is None:
             Qout = torch.empty((N, Hq, D), dtype=t, device=K.device)
-        q = _rows(Q, "Q", K, g, t, (N, Hq, D))
-        qo = _rows(Qout, "Qout", K, g, t, (N, Hq, D))
+        q = _rows(Q, "Q", K, g, t, N, Hq, D)
+        qo = _rows(Qout, "Qout", K, g, t, N, Hq, D)
     B, paged = _paged(Kc, Vc, pages, starts, lens, K, g, t, Hk, D)
     _check("ssn_kv_append", lib().ssn_kv_append(
-        _code(t), N, B, Hq, Hk, D, R, P, code, e, *q, *_rows(K, "K", K, g, t, (N, Hk, D)),
-        *_rows(V, "V", K, g, t, (N, Hk, D)), _weight(wq, "wq", K, g, t, D) if Hq else None,
+        _code(t), N, B, Hq, Hk, D, R, P, code, e, *q, *_rows(K, "K", K, g, t, N, Hk, D),
+        *_rows(V, "V", K, g, t, N, Hk, D), _weight(wq, "wq", K, g, t, D) if Hq else None,
         _weight(wk, "wk", K, g, t, D), _gpu(table, "table", K, g, torch.float32, 2) if R else None,
         *paged, *qo, _stream(stream)))
     return Qout if Q is not None else None
@@ -853,7 +856,7 @@ def paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, pages: 
     B, paged = _paged(Kc, Vc, pages, starts, lens, Q, g, t, Hk, D)
     _check("ssn_paged_attention", lib().ssn_paged_attention(
         _code(t), N, B, Hq, Hk, D, max_q, max_len, D ** -0.5 if scale is None else float(scale),
-        *_rows(Q, "Q", Q, g, t, (N, Hq, D)), *paged, *_rows(out, "out", Q, g, t, (N, Hq, D)),
+        *_rows(Q, "Q", Q, g, t, N, Hq, D), *paged, *_rows(out, "out", Q, g, t, N, Hq, D),
         None if lse is None else _gpu(lse, "lse", Q, g, torch.float32, 2),
         None if workspace is None else _gpu(workspace, "workspace", Q, g, torch.uint8, 1),
         0 if workspace is None else workspace.numel(), _stream(stream)))
