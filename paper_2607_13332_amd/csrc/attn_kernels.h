@@ -29,9 +29,7 @@ __global__ __launch_bounds__(256, (tiles_blocks<T, DT>())) void paged_attn_tiles
   tiles_block<T, DT, QB, EXACT>(a, part, few, count, blockIdx.x, lds);
 }
 
-// Both: the tiles' blocks are bound by the matrix cores, the rows' by memory.
-// They go out in rounds of one tile block to a compute unit and an equal share
-// of the rows' blocks, so that a compute unit has one of each.
+// Both in one launch: first the tiles' blocks, the longer ones.
 template <typename T, int DT>
 constexpr int both_blocks() { return rows_blocks<T, DT, 1>() < tiles_blocks<T, DT>() ? rows_blocks<T, DT, 1>() : tiles_blocks<T, DT>(); }
 template <typename T, int DT, int QB, bool EXACT>
@@ -41,15 +39,9 @@ __global__ __launch_bounds__(256, (both_blocks<T, DT>())) void paged_attn_both(A
   __shared__ __align__(1024) char lds[kLds];
   TileCount count;
   count.count(a.pb, a.G, 64 * QB, p.few, slots);
-  const int tiles = count.total * a.Hk * p.tiles.ranges, rounds = tiles > 0 ? (tiles + kUnits - 1) / kUnits : 1;
-  const int share = (rows + rounds - 1) / rounds, round = blockIdx.x / (kUnits + share);
-  const int at = blockIdx.x - round * (kUnits + share);
-  if (at < kUnits) {
-    if (round * kUnits + at < tiles)
-      tiles_block<T, DT, QB, EXACT>(a, p.tiles, p.few, count, round * kUnits + at, lds);
-  } else if (round * share + at - kUnits < rows) {
-    rows_block<T, DT, 1, EXACT>(a, p.rows, p.few, round * share + at - kUnits, lds);
-  }
+  const int tiles = count.total * a.Hk * p.tiles.ranges, id = blockIdx.x;
+  if (id < tiles) tiles_block<T, DT, QB, EXACT>(a, p.tiles, p.few, count, id, lds);
+  else if (id - tiles < rows) rows_block<T, DT, 1, EXACT>(a, p.rows, p.few, id - tiles, lds);
 }
 
 template <typename T, int DT, int QB, bool EXACT>
@@ -63,10 +55,8 @@ static hipError_t launch_tiles(const AttnArgs& a, const AttnPlan& p, hipStream_t
   const int64_t slots = tile_slots(a.pb.N, a.pb.B, a.G, 64 * QB), tiles = slots * a.Hk * p.tiles.ranges;
   if (p.rows.blocks) {
     const int64_t rows = (int64_t)a.pb.B * a.Hk * p.rows.ranges;
-    // whole rounds, for any number of tiles up to `tiles`
-    const int64_t rounds = (tiles + kUnits - 1) / kUnits;
-    hipLaunchKernelGGL((paged_attn_both<T, DT, QB, EXACT>), dim3((unsigned)(rounds * (kUnits + 1) + rows)), dim3(256),
-                       0, st, a, p, (int)slots, (int)rows);
+    hipLaunchKernelGGL((paged_attn_both<T, DT, QB, EXACT>), dim3((unsigned)(tiles + rows)), dim3(256), 0, st, a, p,
+                       (int)slots, (int)rows);
   } else {
     hipLaunchKernelGGL((paged_attn_tiles<T, DT, QB, EXACT>), dim3((unsigned)tiles), dim3(256), 0, st, a, p.tiles,
                        p.few, (int)slots);

@@ -22,11 +22,17 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kNegInf = -__builtin_inff();
 
 // A cache row in LDS is RB bytes in 16-byte chunks, chunk c of key k at
-// position c ^ swizzle(k): 16 consecutive keys' equal chunks (the K operand)
-// and 4 consecutive keys' 32-byte pieces (the V operand) fall into different
-// banks.
+// position c ^ swizzle(k).  LDS serves 8 lanes' 16 bytes or 16 lanes' 8 bytes a
+// cycle, 128 bytes: of K's rows the equal chunks of 8 consecutive keys have to
+// fall into different columns of 16 bytes, of V's the 32-byte pieces of 4
+// consecutive keys (rocprofv3 counts no conflict; with V's order for both, 30 %
+// of the LDS cycles were conflicts).
 template <int RB>
-__device__ __forceinline__ uint32_t swizzle(uint32_t k) {
+__device__ __forceinline__ uint32_t swizzle_keys(uint32_t k) {
+  return RB >= 256 ? k & 15 : k & 7;
+}
+template <int RB>
+__device__ __forceinline__ uint32_t swizzle_values(uint32_t k) {
   if constexpr (RB >= 256) return ((k & 7) << 1) | ((k >> 3) & 1);
   else return (((k >> 1) & 3) << 1) | ((k >> 3) & 1);
 }
@@ -50,7 +56,7 @@ struct Mma<uint16_t> {
   template <int RB>
   __device__ static __forceinline__ uint32_t vbase(int lane, int) {
     const int L = lane & 15, key = 4 * (lane >> 4) + (L >> 2);
-    return key * RB + ((((uint32_t)(L & 3) >> 1) ^ swizzle<RB>(key)) << 4) + (L & 1) * 8;
+    return key * RB + ((((uint32_t)(L & 3) >> 1) ^ swizzle_values<RB>(key)) << 4) + (L & 1) * 8;
   }
   static constexpr int kBases = 1;
   template <int RB>
@@ -84,7 +90,7 @@ struct Mma<float> {
   template <int RB>
   __device__ static __forceinline__ uint32_t vbase(int lane, int i) {
     const int L = lane & 15, key = 4 * (lane >> 4) + i;
-    return key * RB + (((uint32_t)(L >> 2) ^ swizzle<RB>(key)) << 4) + (L & 3) * 4;
+    return key * RB + (((uint32_t)(L >> 2) ^ swizzle_values<RB>(key)) << 4) + (L & 3) * 4;
   }
   static constexpr int kBases = 4;
   template <int RB>

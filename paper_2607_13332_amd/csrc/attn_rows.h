@@ -97,7 +97,7 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, const AttnPart& pa
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int r = i * RPI + lane / CH;
-      *(u32x4*)(vl + r * RB + (((uint32_t)(lane % CH) ^ swizzle<RB>(r)) << 4)) = vreg[i];
+      *(u32x4*)(vl + r * RB + (((uint32_t)(lane % CH) ^ swizzle_values<RB>(r)) << 4)) = vreg[i];
     }
     wave_lds_order();
     f32x4 s[NKB][QB];

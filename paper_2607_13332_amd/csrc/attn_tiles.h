@@ -10,10 +10,11 @@ namespace ssn {
 typedef __attribute__((address_space(3))) uint32_t lds_word;
 typedef __attribute__((address_space(1))) const uint32_t global_word;
 
-// The launch's row tiles.  Up to kCounted sequences every block counts them
-// (a wave scans the row counts), so that the tiles there are come first in the
-// grid; past that sequence b has the numbers from starts[b] * G / BM + b on,
-// which leaves ceil(rows / BM) to each, and some numbers name none.
+// The launch's row tiles, those that see the most keys first: a sequence's last
+// tile sees the most.  Up to kCounted sequences every block counts the tiles of
+// each (four a lane) and ranks them by their place in their sequence; past that
+// sequence b has the numbers from starts[b] * G / BM + b on, which leaves ceil(rows
+// / BM) to each, some numbers name none, and the last goes first.
 constexpr int kCounted = 256;
 inline int64_t tile_slots(int64_t N, int64_t B, int64_t G, int64_t BM) { return N * G / BM + B; }
 __device__ __forceinline__ int first_slot(const PagedBatch& pb, int b, int G, int BM) {
@@ -26,57 +27,81 @@ __device__ __forceinline__ int tiles_of(const PagedBatch& pb, int b, int G, int 
 }
 struct TileCount {
   int mine[kCounted / kWave];     // tiles of sequence 64 c + lane
-  int total;
+  int total, most;
+  // The sum over a wave of values below 2^bits, in scalar registers: bit by bit,
+  // by the lanes that have it.
+  __device__ __forceinline__ static int wave_total(int v, int bits) {
+    int n = 0;
+    for (int k = 0; k < bits; ++k) n += __popcll(__ballot((v >> k) & 1)) << k;
+    return n;
+  }
+  __device__ __forceinline__ static int bits_of(int v) { return 32 - __clz(v); }
   __device__ __forceinline__ void count(const PagedBatch& pb, int G, int BM, int few, int slots) {
-    if (pb.B > kCounted) {
-      total = slots;
+    total = slots;
+    if (pb.B > kCounted) return;
+    if (pb.B == 1) {
+      total = tiles_of(pb, 0, G, BM, few);
       return;
     }
+#pragma unroll
+    for (int c = 0; c < kCounted / kWave; ++c)
+      mine[c] = 64 * c < pb.B ? tiles_of(pb, 64 * c + (threadIdx.x & 63), G, BM, few) : 0;
+    most = 0;
+    for (int k = bits_of(slots) - 1; k >= 0; --k) {
+      const int up = (most | (1 << k)) >> k;
+      bool has = false;
+#pragma unroll
+      for (int c = 0; c < kCounted / kWave; ++c) has |= (mine[c] >> k) == up;
+      if (__any(has)) most |= 1 << k;
+    }
+    // contents past the contract may count more than the grid has
+    const int n = from_level(0);
+    total = n < slots ? n : slots;
+  }
+  // Tiles that are number `level` or later of their sequence.
+  __device__ __forceinline__ int from_level(int level) const {
     int n = 0;
 #pragma unroll
-    for (int c = 0; c < kCounted / kWave; ++c) {
-      mine[c] = 64 * c < pb.B ? tiles_of(pb, 64 * c + (threadIdx.x & 63), G, BM, few) : 0;
-      n += mine[c];
-    }
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) n += __shfl_xor(n, m, kWave);
-    // contents past the contract may count more than the grid has
-    total = __builtin_amdgcn_readfirstlane(n < slots ? n : slots);
+    for (int c = 0; c < kCounted / kWave; ++c) n += mine[c] > level ? mine[c] - level : 0;
+    return wave_total(n, bits_of(most) + 2);
   }
-  // Sequence and tile of it of number i < total; false: none.
+  // Sequence and tile of rank i < total; false: none.
   __device__ __forceinline__ bool find(const PagedBatch& pb, int G, int BM, int few, int i, int& b, int& tile) const {
     if (pb.B > kCounted) {
-      b = last_at_most(pb.B, i, [&](int x) { return first_slot(pb, x, G, BM); });
-      tile = i - first_slot(pb, b, G, BM);
+      const int slot = total - 1 - i;
+      b = last_at_most(pb.B, slot, [&](int x) { return first_slot(pb, x, G, BM); });
+      tile = slot - first_slot(pb, b, G, BM);
       return tile >= 0 && tile < tiles_of(pb, b, G, BM, few);
     }
-    int before = 0;
+    if (pb.B == 1) {
+      b = 0;
+      tile = total - 1 - i;
+      return true;
+    }
+    int lo = 0, hi = most;          // from_level(lo) > i >= from_level(hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (from_level(mid) > i) lo = mid;
+      else hi = mid;
+    }
+    tile = lo;
+    int nth = i - from_level(lo + 1);
     const int lane = threadIdx.x & 63;
-    for (int c = 0; c < kCounted / kWave; ++c) {
-      int sum = c == 0 ? mine[0] : (c == 1 ? mine[1] : (c == 2 ? mine[2] : mine[3]));
-      const int own = sum;
 #pragma unroll
-      for (int m = 1; m < kWave; m <<= 1) {
-        const int x = __shfl_up(sum, m, kWave);
-        if (lane >= m) sum += x;
-      }
-      const uint64_t hit = __ballot(before + sum > i);
-      if (hit) {
-        const int l = __ffsll((unsigned long long)hit) - 1;
-        b = 64 * c + l;
-        tile = i - before - (__shfl(sum, l, kWave) - __shfl(own, l, kWave));
-        b = __builtin_amdgcn_readfirstlane(b);
-        tile = __builtin_amdgcn_readfirstlane(tile);
+    for (int c = 0; c < kCounted / kWave; ++c) {
+      const uint64_t has = __ballot(mine[c] > lo);
+      const int n = __popcll(has), rank = __popcll(has & (((uint64_t)1 << lane) - 1));
+      if (nth < n) {
+        b = 64 * c + __ffsll((unsigned long long)__ballot(mine[c] > lo && rank == nth)) - 1;
         return true;
       }
-      before += __shfl(sum, 63, kWave);
+      nth -= n;
     }
     return false;
   }
 };
 
-// A sequence's last tiles see the most keys, so they go first; and a compute
-// unit, which gets one block of the first round and one of the second, gets a
+// A compute unit gets one block of the first round and one of the second: a
 // long and a short one.
 constexpr int kUnits = 256;
 __device__ __forceinline__ int balanced_order(int i, int slots, int Hk) {
@@ -162,7 +187,7 @@ __device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& p
   const int range = rest / count.total;
   int b, tile;
   if (range >= part.ranges ||
-      !count.find(a.pb, a.G, BM, few, count.total - 1 - balanced_order(rest % count.total, count.total, a.Hk), b, tile))
+      !count.find(a.pb, a.G, BM, few, balanced_order(rest % count.total, count.total, a.Hk), b, tile))
     return;
   const Sequence sq = sequence_of(a.pb, b);
   const int n = sq.s1 - sq.s0, rows = n * a.G, r0 = tile * BM;
@@ -203,12 +228,12 @@ __device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& p
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int base = (i * 4 + wave) * RPI, r = base + lane / CH;
-      const uint32_t chunk = (uint32_t)(lane % CH) ^ swizzle<RB>(r);
-      const int64_t src = (int64_t)(uint32_t)__shfl((int)mine, r, kWave) * bytes + chunk * 16;
-      if (EXACT || (int)chunk * 16 < bytes) {
-        __builtin_amdgcn_global_load_lds((global_word*)((const char*)a.Kc + src), (lds_word*)&lds[buf][0][base * RB], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_word*)((const char*)a.Vc + src), (lds_word*)&lds[buf][1][base * RB], 16, 0, 0);
-      }
+      const uint32_t kc = (uint32_t)(lane % CH) ^ swizzle_keys<RB>(r), vc = (uint32_t)(lane % CH) ^ swizzle_values<RB>(r);
+      const int64_t src = (int64_t)(uint32_t)__shfl((int)mine, r, kWave) * bytes;
+      if (EXACT || (int)kc * 16 < bytes)
+        __builtin_amdgcn_global_load_lds((global_word*)((const char*)a.Kc + src + kc * 16), (lds_word*)&lds[buf][0][base * RB], 16, 0, 0);
+      if (EXACT || (int)vc * 16 < bytes)
+        __builtin_amdgcn_global_load_lds((global_word*)((const char*)a.Vc + src + vc * 16), (lds_word*)&lds[buf][1][base * RB], 16, 0, 0);
     }
   };
   if constexpr (!EXACT) {
@@ -220,7 +245,7 @@ __device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& p
   uint32_t vb[M::kBases];
 #pragma unroll
   for (int i = 0; i < M::kBases; ++i) vb[i] = M::template vbase<RB>(lane, i);
-  const uint32_t kb0 = (lane & 15) * RB + (((uint32_t)(lane >> 4) ^ swizzle<RB>(lane & 15)) << 4);
+  const uint32_t kb0 = (lane & 15) * RB + (((uint32_t)(lane >> 4) ^ swizzle_keys<RB>(lane & 15)) << 4);
 
   RowState<DT / 16, QB> rs;
   rs.clear();
