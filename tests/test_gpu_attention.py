@@ -475,3 +475,71 @@ def test_wrappers_refuse():
     with pytest.raises(ValueError, match="GPU tensor"):
         c = torch.zeros((4, 4, 64))
         ssn.qk_norm_rope(c, c)
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("dtype,Hq,Hk,D", [("bf16", 4, 2, 64), ("bf16", 10, 2, 128), ("bf16", 3, 1, 112),
+                                           ("f32", 4, 2, 64), ("f32", 2, 1, 128), ("bf16", 2, 2, 256)])
+def test_chunks_over_long_caches(dtype, Hq, Hk, D, split):
+    """The widest row tiles, with and without key ranges, beside a single
+    token and a prompt."""
+    bt = Batch([(100, 8300), (1, 8200), (90, 100), (17, 17)], Hk, D, 48, dtype, 2, first=1, pad=2)
+    q, out, lse = _attend(bt, Hq, Hk, D, dtype, 4, split)
+    _check_attention(bt, Hq, Hk, D, dtype, q, out, lse)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("at", [0, 70, 139])
+def test_unseen_infinities_under_wide_tiles(dtype, D, at):
+    new, length = 140, 8200
+    bt, bad = (Batch([(new, length), (1, 30)], 1, D, 16, dtype, 5) for _ in range(2))
+    q, clean, _ = _attend(bt, 2, 1, D, dtype, 2)
+    page, off = bad.slots(0)
+    for j in range(length - new + at, length):
+        bad.Vc[page[j], :, off[j], j % D] = poison(dtype)[j % 3]
+        if j % 5 == 0:
+            bad.Kc[page[j], :, off[j]] = poison(dtype)[j % 3]
+    _, out, _ = _attend(bad, 2, 1, D, dtype, 2, q=q)
+    assert np.array_equal(out[:at], clean[:at]) and np.array_equal(out[new:], clean[new:])
+    # the row of position j sees the infinity of its own value
+    got = f64(out)
+    for i in range(at, new):
+        assert not np.isfinite(got[i, :, (length - new + i) % D]).any(), i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [65, 200, 256, 300, 1000])
+def test_many_sequences(dtype, B):
+    """Ragged batches on both sides of the count up to which tiles are ranked,
+    with bounds above what is in them."""
+    r = np.random.default_rng(B)
+    seqs = []
+    for b in range(B):
+        n = int(r.choice([0, 1, 1, 2, 5, 33, 70]))
+        seqs.append((n, n + int(r.integers(0, 60)) if r.random() < 0.9 else 1))
+    bt = Batch(seqs, 2, 64, 16, dtype, 3, first=5, pad=4)
+    bt.max_q, bt.max_len = 200, 500
+    q, out, lse = _attend(bt, 8, 2, 64, dtype, 1)
+    _check_attention(bt, 8, 2, 64, dtype, q, out, lse)
+
+
+def test_bounds_below_the_contents_stay_in_bounds():
+    """max_q and max_len below what the batch holds, row ranges past N, page
+    numbers out of range: unspecified results, no access outside the buffers
+    (guard rows around the output keep their values)."""
+    bt = Batch([(5, 300), (40, 90), (1, 1000)], 2, 64, 16, "bf16", 3)
+    Kc, Vc, pages, starts, lens = bt.device()
+    Q = torch.zeros((bt.N, 8, 64), dtype=torch.bfloat16, device=DEV)
+    guard = torch.full((bt.N + 64, 8, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = guard[32:32 + bt.N]
+    for max_q, max_len in [(1, 10), (3, 1000), (40, 100)]:
+        ws = ssn.paged_attention_workspace(bt.N, 3, 8, 2, 64, max_q, max_len, DEV)
+        ssn.paged_attention(Q, Kc, Vc, pages, starts, lens, max_q, max_len, out=out, workspace=ws)
+    far = torch.tensor([0, 10 ** 6, -5, 10 ** 9], dtype=torch.int32, device=DEV)
+    ssn.paged_attention(Q, Kc, Vc, pages, far, lens * 1000, 40, 10 ** 6, out=out)
+    ssn.paged_attention(Q, Kc, Vc, torch.full_like(pages, -7), starts, lens, 40, 1000, out=out)
+    K = torch.zeros((bt.N, 2, 64), dtype=torch.bfloat16, device=DEV)
+    ssn.kv_append(K, K.clone(), Kc, Vc, pages, far, lens * 1000)
+    ssn.kv_append(K, K.clone(), Kc, Vc, torch.full_like(pages, 10 ** 9), starts, lens)
+    torch.cuda.synchronize()
+    assert (guard[:32] == 7).all() and (guard[32 + bt.N:] == 7).all()
