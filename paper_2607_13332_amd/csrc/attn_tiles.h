@@ -7,8 +7,16 @@
 
 namespace ssn {
 
-typedef __attribute__((address_space(3))) uint32_t lds_word;
-typedef __attribute__((address_space(1))) const uint32_t global_word;
+// 16 bytes of every active lane, from its own address to LDS: lane i's to `to` +
+// 16 i (`to` the same in the wave).  In assembly, because the compiler waits for
+// all such loads before the next ds_read_b64_tr_b16, also where that reads
+// another buffer (2048-token prompt 62 -> 59 us, 4 of 4096 686 -> 674); there is
+// no output register.  Readers wait for vmcnt and pass a barrier.
+__device__ __forceinline__ void load_to_lds(const char* from, const char* to) {
+  const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)to;
+  // (one wait state between a scalar write of m0 and its use by the load)
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(at) : "memory");
+}
 
 // The launch's row tiles, those that see the most keys first: a sequence's last
 // tile sees the most.  Up to kCounted sequences every block counts the tiles of
@@ -231,9 +239,9 @@ __device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& p
       const uint32_t kc = (uint32_t)(lane % CH) ^ swizzle_keys<RB>(r), vc = (uint32_t)(lane % CH) ^ swizzle_values<RB>(r);
       const int64_t src = (int64_t)(uint32_t)__shfl((int)mine, r, kWave) * bytes;
       if (EXACT || (int)kc * 16 < bytes)
-        __builtin_amdgcn_global_load_lds((global_word*)((const char*)a.Kc + src + kc * 16), (lds_word*)&lds[buf][0][base * RB], 16, 0, 0);
+        load_to_lds((const char*)a.Kc + src + kc * 16, &lds[buf][0][base * RB]);
       if (EXACT || (int)vc * 16 < bytes)
-        __builtin_amdgcn_global_load_lds((global_word*)((const char*)a.Vc + src + vc * 16), (lds_word*)&lds[buf][1][base * RB], 16, 0, 0);
+        load_to_lds((const char*)a.Vc + src + vc * 16, &lds[buf][1][base * RB]);
     }
   };
   if constexpr (!EXACT) {
