@@ -2,6 +2,12 @@
 // 4 waves owns a range of the keys of one sequence and key head; its waves take
 // the range's tiles in turn, all with the same 16 QB rows, and join their
 // results in LDS at the end.
+//
+// What bounds it: reading the cache.  64 single tokens over caches of 1 to 4096
+// keys (40 / 8 heads of 128, bf16) take 98 us (5.6 TB/s), four over 100000 to
+// 131072 keys 314 us (6.7 TB/s; a large copy moves 4.6), and the join 7 to 9 us
+// more.  The matrix cores are used with 16 rows where a group has 4 or 5 heads:
+// they are busy 4 % of the time, and each key is read once for the group.
 #pragma once
 
 #include "attn_tiles.h"

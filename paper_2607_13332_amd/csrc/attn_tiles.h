@@ -1,6 +1,18 @@
 // Paged attention of many rows: a block of 4 waves owns a tile of rows of one
 // sequence and key head (64 QB rows, 16 QB to a wave) and walks the keys the
-// tile sees.
+// tile sees, 64 (or 32) at a time through LDS, double buffered.  Rows of all the
+// heads of a group share the tile, so a key is read once for the group.
+//
+// What bounds it: the compute.  A prompt of 4096 tokens (40 / 8 heads of 128, bf16)
+// takes 171 us, 1010 TFLOP/s where a large matrix product reaches 1260 to 1365, and
+// four of them 680 us, 1010.  Of that the matrix cores are busy 40 %, the vector
+// units issue 45 %; without the tile loads it would take 12 % less, without the
+// exponentials 4 %, without barriers the same: the rest is the latency of
+// LDS reads, products and probabilities one after the other in a wave, two waves
+// to a SIMD.  Measured and not kept: scores a step ahead of the probabilities (+-5
+// %), values read before the scores (+-2 %), 32-key tiles with three blocks to a
+// compute unit (spills), blocks of 8 waves (1 to 5 % faster at 4096 tokens and
+// more, 10 % slower below).
 #pragma once
 
 #include "attn_mma.h"

@@ -246,11 +246,16 @@ static AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int6
   if (tiles) {
     const int64_t rows = (p.few && N - B >= 0 ? N - B + 1 : N) * G;
     p.tiles.blocks = tile_rows(dtype, rows, most, Hk, D, max_len);
-    // two blocks to a compute unit, where the rows alone do not give them
+    // two blocks to a compute unit, where the rows alone do not give them (512
+    // tokens over 32768 keys: 497 us for 256 blocks, 317 for 512, 315 for 1024;
+    // four chunks of up to 100 over 8192: 105, 76, 87)
     const int64_t blocks = (rows / (64 * p.tiles.blocks) + 1) * Hk;
     split_keys(p.tiles, blocks >= 512 ? 1 : 512 / blocks, 256, max_len, D, ws_bytes);
   }
   if (p.rows.blocks) {
+    // about 2048 blocks, so that long and short caches spread evenly (64 caches of
+    // 1 to 4096 keys: 125 / 116 / 105 / 107 / 120 us for 512 / 1024 / 2048 / 4096 /
+    // 8192), and no more than 64 ranges to join where 512 blocks have them
     const size_t left = ws_bytes - stage_bytes(p.tiles, D);
     const int64_t pairs = B * Hk, full = 512 / pairs, want = (2048 + pairs - 1) / pairs;
     split_keys(p.rows, want > 64 && want > full ? (full > 64 ? full : 64) : want, 128, max_len, D, left);
