@@ -473,9 +473,10 @@ ssn_status_t ssn_delta_rule(int64_t n, int64_t m, const int64_t *I, int64_t firs
  * stride `ld` in elements (ld >= H * D), the heads of a row packed, so that
  * queries, keys and values may be parts of one [N, ld] projection.  Outputs
  * may be parts of one buffer as well; they must not overlap inputs or each
- * other.  The kernels' fast paths need D = 64, 128 or 256, 16-byte aligned
- * pointers and row strides of a multiple of 16 bytes; other shapes (D <= 1024,
- * else SSN_ERR_UNSUPPORTED) run the generic kernels.
+ * other.  The kernels' fast paths need 16-byte aligned pointers and row strides
+ * of a multiple of 16 bytes, and for norms and appends D = 64, 128 or 256, R = D
+ * or 0; for attention any D <= 256 whose rows are a multiple of 16 bytes.  Other
+ * shapes (D <= 1024, else SSN_ERR_UNSUPPORTED) run the generic kernels.
  *
  * Rotation: `table` [P, R] float32 holds in row p the R / 2 cosines and then
  * the R / 2 sines of position p; R is even, 0 <= R <= D (0: no rotation, the

@@ -318,6 +318,9 @@ struct Spread {
   int passes, slots;
   __host__ __device__ int64_t waves() const { return (int64_t)passes * slots; }
 };
+// (max_waves for the forward: appends of 11425 tokens take 88 / 82 / 72 / 69 / 76
+// us for 4096 / 8192 / 16384 / 32768 / 131072 waves; the norms alone do not mind)
+constexpr int64_t kForwardWaves = 32768;
 static Spread spread_tokens(int64_t N, int heads, int heads_per_wave, int64_t max_waves) {
   Spread s;
   s.passes = (heads + heads_per_wave - 1) / heads_per_wave;
@@ -326,8 +329,10 @@ static Spread spread_tokens(int64_t N, int heads, int heads_per_wave, int64_t ma
   return s;
 }
 
+// 4096 tokens of 40 + 8 heads of 128, bf16: 20.5 us, 5.0 TB/s.
 // APPEND: keys and values go to their slots of the cache, positions follow
-// from the batch, and the heads of v come after those of k.
+// from the batch, and the heads of v come after those of k.  Four prompts of
+// 11425 tokens in all: 69 us, 5.3 TB/s; one token 3.2 us.
 template <typename T, int D, int ROT, bool APPEND>
 __global__ __launch_bounds__(256) void norm_rope_rows(int N, Spread sp, NormRope nr, HeadRows q, HeadRows k,
                                                       HeadRows v, const T* __restrict__ wq,
@@ -401,6 +406,8 @@ __global__ __launch_bounds__(256) void norm_rope_rows(int N, Spread sp, NormRope
   }
 }
 
+// 12205 tokens of 40 + 8 heads of 128, bf16: 76 us, 5.9 TB/s, and 4.8 us for the
+// sum of the blocks' shares of dL/dw.
 constexpr int kBackWaves = 8;         // of a block
 template <typename T, int D, int ROT>
 __global__ __launch_bounds__(64 * kBackWaves) void norm_rope_backward_rows(
@@ -452,14 +459,15 @@ __global__ __launch_bounds__(64 * kBackWaves) void norm_rope_backward_rows(
         dot += a.v[e] * wa.v[e] * xa.v[e] + b.v[e] * wb.v[e] * xb.v[e];
       }
       const float r = rsqrtf(head_sum<LPH>(ss) * (1.f / D) + nr.eps);
-      // x r times the mean of h x r, times r
-      const float m = head_sum<LPH>(dot) * (1.f / D) * r * r * r;
+      // mean(h x r) r; r^3 by itself could leave float32 (heads of 1e-18, no eps)
+      const float m = head_sum<LPH>(dot) * r * (1.f / D) * r;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        ga.v[e] += a.v[e] * (xa.v[e] * r);
-        gb.v[e] += b.v[e] * (xb.v[e] * r);
-        a.v[e] = a.v[e] * wa.v[e] * r - xa.v[e] * m;
-        b.v[e] = b.v[e] * wb.v[e] * r - xb.v[e] * m;
+        const float na = xa.v[e] * r, nb = xb.v[e] * r;
+        ga.v[e] += a.v[e] * na;
+        gb.v[e] += b.v[e] * nb;
+        a.v[e] = a.v[e] * wa.v[e] * r - na * m;
+        b.v[e] = b.v[e] * wb.v[e] * r - nb * m;
       }
     }
     if (any) {
@@ -521,7 +529,8 @@ struct RowsLaunch {
 };
 template <typename T, int D, int ROT, bool APPEND>
 static hipError_t launch_rows_kernel(const RowsLaunch& a) {
-  const Spread sp = spread_tokens(a.N, a.q.H + (APPEND ? 2 : 1) * a.k.H, kWave * 2 * Chunk<T>::E / D, 32768);
+  const Spread sp = spread_tokens(a.N, a.q.H + (APPEND ? 2 : 1) * a.k.H, kWave * 2 * Chunk<T>::E / D,
+                                  kForwardWaves);
   hipLaunchKernelGGL((norm_rope_rows<T, D, ROT, APPEND>), dim3((unsigned)((sp.waves() + 3) / 4)), dim3(256), 0,
                      a.st, (int)a.N, sp, a.nr, a.q, a.k, a.v, (const T*)a.wq, (const T*)a.wk, a.pos, a.qo, a.ko,
                      a.pb, (T*)a.Kc, (T*)a.Vc);
@@ -594,8 +603,9 @@ hipError_t launch_norm_rope(int dtype, int64_t N, const NormRope& nr, HeadRows q
   return hipGetLastError();
 }
 
-// Enough waves for two blocks of 8 on every compute unit, and few enough
-// partial sums that adding them costs nothing.
+// Two blocks of 8 waves on every compute unit: 12205 tokens of 48 heads of 128
+// take 147 / 89 / 80 / 84 / 90 us (with the sum over blocks) for 128 / 256 / 512 /
+// 1024 / 2048 blocks, 2000 tokens 31 / 23 / 22 / 29 / 40.
 int norm_rope_backward_blocks(int64_t N, int64_t heads) {
   const int64_t b = (N * heads + 31) / 32;
   return (int)(b < 1 ? 1 : (b > 512 ? 512 : b));

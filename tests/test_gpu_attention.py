@@ -543,3 +543,23 @@ def test_bounds_below_the_contents_stay_in_bounds():
     ssn.kv_append(K, K.clone(), Kc, Vc, torch.full_like(pages, 10 ** 9), starts, lens)
     torch.cuda.synchronize()
     assert (guard[:32] == 7).all() and (guard[32 + bt.N:] == 7).all()
+
+
+@pytest.mark.parametrize("D", [64, 128, 96])
+def test_norm_backward_of_tiny_and_large_heads(D):
+    """Without eps, a head of 1e-18 under gradients of 1e5: the gradient (1e23) is a
+    float32 number, the mean of h x times the third power of the inverse root mean
+    square (1e41) is not.
+
+    Bound: sums of at most 128 terms in registers and exchanges round some 20 times,
+    the inverse root and the products 10 times more; 30 x 2^-24 = 2e-6 of the head's
+    norm, and 1e-5 leaves a factor of five."""
+    r = np.random.default_rng(1)
+    x = r.standard_normal((3, 2, D)) * np.array([1e-18, 1.0, 1e16])[:, None, None]
+    gy = r.standard_normal((3, 2, D)) * np.array([1e5, 1.0, 1.0])[:, None, None]
+    x, gy = x.astype(np.float32), gy.astype(np.float32)
+    X, G = torch.from_numpy(x).to(DEV), torch.from_numpy(gy).to(DEV)
+    got, _, _, _ = ssn.qk_norm_rope_backward(X, X, G, G, eps=0.0)
+    ref, _ = A.norm_rope_backward(x, gy, None, None, None, 0.0)
+    for i in range(3):
+        assert rel(got[i].cpu().numpy(), ref[i]) <= 1e-5, i
