@@ -458,7 +458,9 @@ __global__ __launch_bounds__(64 * kBackWaves) void norm_rope_backward_rows(
         ss += xa.v[e] * xa.v[e] + xb.v[e] * xb.v[e];
         dot += a.v[e] * wa.v[e] * xa.v[e] + b.v[e] * wb.v[e] * xb.v[e];
       }
-      const float r = rsqrtf(head_sum<LPH>(ss) * (1.f / D) + nr.eps);
+      // (a lane without a head holds zeros: at eps = 0 their inverse root would be
+      // infinite, and its products NaN in the shares of dL/dw)
+      const float inv = rsqrtf(head_sum<LPH>(ss) * (1.f / D) + nr.eps), r = any ? inv : 0.f;
       // mean(h x r) r; r^3 by itself could leave float32 (heads of 1e-18, no eps)
       const float m = head_sum<LPH>(dot) * r * (1.f / D) * r;
 #pragma unroll
