@@ -658,6 +658,8 @@ def _rows(t: torch.Tensor, name: str, first: torch.Tensor, dev: int, dtype, N: i
     if t.shape != (N, H, D):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(N, H, D)}")
     ld, sh, se = t.stride()
+    if N == 0 or H == 0:               # nothing is read: any strides
+        return t.data_ptr(), H * D
     if N <= 1:
         ld = H * D
     if (se != 1 and D > 1) or (sh != D and H > 1) or ld < H * D:

@@ -1,0 +1,37 @@
+"""The attention sublayer's calls at the edges of their contract."""
+import numpy as np
+import pytest
+import torch
+
+from attn_helpers import DEV, Batch, dev
+from oracle import attn_oracle as A
+from paper_2607_13332_amd import inputs as I
+from paper_2607_13332_amd import ssn
+
+pytestmark = pytest.mark.gpu
+
+
+def _nothing(*shape):
+    """A tensor without elements whose strides are all zero (as numpy's are)."""
+    return torch.empty(0, dtype=torch.bfloat16, device=DEV).as_strided(shape, (0, 0, 0))
+
+
+def test_sides_without_heads_and_batches_without_rows():
+    """Tensors without elements are taken whatever their strides are."""
+    r = np.random.default_rng(0)
+    x = I.store(r.standard_normal((3, 2, 64)), "bf16")
+    X, none = dev(x, "bf16"), _nothing(3, 0, 64)
+    Q, K = ssn.qk_norm_rope(X, none)
+    K2 = ssn.qk_norm_rope(none, X)[1]
+    ref = A.norm_rope(x)
+    assert K.shape == (3, 0, 64) and torch.equal(Q, K2)
+    assert np.abs(Q.double().cpu().numpy() - ref).max() <= 2.0 ** -8 * np.abs(ref).max()
+    GQ, GK, _, _ = ssn.qk_norm_rope_backward(X, none, X, none)
+    assert GK.shape == (3, 0, 64) and torch.equal(GQ, ssn.qk_norm_rope_backward(none, X, none, X)[1])
+    bt = Batch([(0, 5)], 2, 64, 16, "bf16", 1)
+    Kc, Vc, pages, starts, lens = bt.device()
+    empty = _nothing(0, 2, 64)
+    before = Kc.clone()
+    assert ssn.kv_append(empty, empty, Kc, Vc, pages, starts, lens) is None
+    assert torch.equal(Kc.view(torch.int16), before.view(torch.int16))
+    assert ssn.paged_attention(_nothing(0, 4, 64), Kc, Vc, pages, starts, lens, 0, 5).shape == (0, 4, 64)
