@@ -313,7 +313,7 @@ __device__ __forceinline__ float head_sum(float v) {
 }
 
 // Waves of a launch: `passes` for each of `slots` tokens; a wave goes on to
-// token + slots.
+// token + slots.  A wave does not change its pass: a launch has waves() of them.
 struct Spread {
   int passes, slots;
   __host__ __device__ int64_t waves() const { return (int64_t)passes * slots; }
@@ -607,10 +607,13 @@ hipError_t launch_norm_rope(int dtype, int64_t N, const NormRope& nr, HeadRows q
 
 // Two blocks of 8 waves on every compute unit: 12205 tokens of 48 heads of 128
 // take 147 / 89 / 80 / 84 / 90 us (with the sum over blocks) for 128 / 256 / 512 /
-// 1024 / 2048 blocks, 2000 tokens 31 / 23 / 22 / 29 / 40.
+// 1024 / 2048 blocks, 2000 tokens 31 / 23 / 22 / 29 / 40.  And a wave for every
+// pass of a token at least: of float32 heads of 256 a wave covers two, a block 16
+// (this counts for one token, and past 8192 heads).
 int norm_rope_backward_blocks(int64_t N, int64_t heads) {
-  const int64_t b = (N * heads + 31) / 32;
-  return (int)(b < 1 ? 1 : (b > 512 ? 512 : b));
+  const int64_t even = (N * heads + 31) / 32, b = even < 512 ? even : 512;
+  const int64_t least = (heads + 2 * kBackWaves - 1) / (2 * kBackWaves);
+  return (int)(b > least ? b : least);
 }
 
 hipError_t launch_norm_rope_backward(int dtype, int64_t N, const NormRope& nr, HeadRows q, HeadRows k,

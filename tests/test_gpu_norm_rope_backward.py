@@ -56,3 +56,24 @@ def test_weight_gradients_without_eps(dtype, Hq, Hk, D, odd, style):
     # N tokens of at most Hq or Hk heads each, one after the other at worst
     _check(dtype, q, gq, wq, pos, table, 0.0, style, GQ, Gwq, N * Hq)
     _check(dtype, k, gk, wk, pos, table, 0.0, style, GK, Gwk, N * Hk)
+
+
+@pytest.mark.parametrize("N,dtype,Hq,Hk,D", [(1, "f32", 16, 1, 256), (1, "f32", 16, 4, 256), (1, "f32", 40, 8, 256),
+                                             (1, "f32", 17, 0, 256), (1, "f32", 0, 17, 256), (1, "bf16", 40, 8, 256),
+                                             (1, "f32", 40, 8, 128), (2, "f32", 9000, 500, 256),
+                                             (1, "bf16", 17000, 100, 256), (1, "f32", 17000, 100, 128)])
+def test_every_head_of_a_few_tokens(N, dtype, Hq, Hk, D):
+    """More heads than 16 waves hold, and more than the waves of 512 blocks:
+    every head's gradient is written (the outputs hold something else before),
+    and the weight gradients have all terms."""
+    q, k, gq, gk, wq, wk, pos, table = _inputs(dtype, Hq, Hk, D, N, 6)
+    print(f"[case] norm backward, many heads: {dtype} N={N} {Hq}/{Hk} x {D}", flush=True)
+    GQ, GK = (torch.full((N, h, D), 7e6, dtype=TORCH[dtype], device=DEV) for h in (Hq, Hk))
+    _, _, Gwq, Gwk = ssn.qk_norm_rope_backward(
+        dev(q, dtype), dev(k, dtype), dev(gq, dtype), dev(gk, dtype), torch.from_numpy(pos).to(DEV),
+        torch.from_numpy(table).to(DEV), dev(wq, dtype), dev(wk, dtype), GQin=GQ, GKin=GK)
+    # a wave's heads and tokens, a block's waves, the blocks' shares 16 at a time
+    if Hq:
+        _check(dtype, q, gq, wq, pos, table, 1e-6, "halves", GQ, Gwq, 60 + N * Hq // 64)
+    if Hk:
+        _check(dtype, k, gk, wk, pos, table, 1e-6, "halves", GK, Gwk, 60 + N * (Hq + Hk) // 64)
