@@ -201,9 +201,11 @@ static hipError_t launch_join(int dtype, const AttnArgs& a, const AttnPlan& p, h
   return hipGetLastError();
 }
 
-// How a call is run.  ws: the workspace (NULL: as many bytes as it takes).
+// Bytes of a part's partial results.  The tiles' lie before the rows', and both
+// are read 16 bytes at a time: a multiple of 16.
 static size_t stage_bytes(const AttnPart& p, int64_t D) {
-  return p.blocks && p.ranges > 1 ? (size_t)p.ranges * (size_t)p.stage_rows * (size_t)(D + 2) * 4 : 0;
+  if (!p.blocks || p.ranges <= 1) return 0;
+  return ((size_t)p.ranges * (size_t)p.stage_rows * (size_t)(D + 2) * 4 + 15) / 16 * 16;
 }
 // Ranges for about `want` of them, no more than `fit` bytes hold.
 static void split_keys(AttnPart& p, int64_t want, int64_t unit, int64_t max_len, int64_t D, size_t fit) {
@@ -234,6 +236,7 @@ static int tile_rows(int dtype, int64_t rows, int64_t most, int64_t Hk, int64_t 
 static AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
                                int64_t max_len, size_t ws_bytes) {
   AttnPlan p = {};
+  ws_bytes = ws_bytes / 16 * 16;
   const int64_t G = Hq / Hk, most = max_q * G;
   const bool tiles = most > 32 || (most > 16 && D > 128);
   // the rows kernel takes all sequences, or the single tokens among longer
@@ -288,12 +291,12 @@ hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void* ws, size_t
     return hipGetLastError();
   }
   AttnPlan p = attention_plan(dtype, a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0);
-  float* at = (float*)ws;
+  char* at = (char*)ws;
   for (AttnPart* x : {&p.tiles, &p.rows})
-    if (stage_bytes(*x, a.D)) {
-      x->o = at;
-      x->ml = at + x->ranges * x->stage_rows * a.D;
-      at = x->ml + x->ranges * x->stage_rows * 2;
+    if (const size_t bytes = stage_bytes(*x, a.D)) {
+      x->o = (float*)at;
+      x->ml = x->o + x->ranges * x->stage_rows * a.D;
+      at += bytes;
     }
   hipError_t e;
   if (p.tiles.blocks) e = dtype == kBF16 ? launch_attn_tiles_bf16(a, p, st) : launch_attn_tiles_f32(a, p, st);

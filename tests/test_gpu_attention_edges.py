@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from attn_helpers import DEV, Batch, dev
+from attn_helpers import DEV, TORCH, Batch, attention_bound, check_close, dev
 from oracle import attn_oracle as A
 from paper_2607_13332_amd import inputs as I
 from paper_2607_13332_amd import ssn
@@ -35,3 +35,21 @@ def test_sides_without_heads_and_batches_without_rows():
     assert ssn.kv_append(empty, empty, Kc, Vc, pages, starts, lens) is None
     assert torch.equal(Kc.view(torch.int16), before.view(torch.int16))
     assert ssn.paged_attention(_nothing(0, 4, 64), Kc, Vc, pages, starts, lens, 0, 5).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_staged_parts_with_an_odd_number_of_rows(dtype):
+    """A chunk and single tokens, both in ranges: 519 x 7 rows times 7 ranges of
+    the tiles' results lie before those of the single tokens."""
+    Hq, D = 7, 128
+    bt = Batch([(517, 7000), (1, 7000), (1, 3)], 1, D, 64, dtype, 2)
+    assert ssn.paged_attention_workspace_bytes(bt.N, 3, Hq, 1, D, bt.max_q, bt.max_len, TORCH[dtype]) > 0
+    r = np.random.default_rng(1)
+    q = I.store(1.5 * r.standard_normal((bt.N, Hq, D)), dtype)
+    Kc, Vc, pages, starts, lens = bt.device()
+    ws = ssn.paged_attention_workspace(bt.N, 3, Hq, 1, D, bt.max_q, bt.max_len, DEV, dtype=TORCH[dtype])
+    ws.fill_(255)
+    out = ssn.paged_attention(dev(q, dtype), Kc, Vc, pages, starts, lens, bt.max_q, bt.max_len, workspace=ws)
+    O, _, M = A.paged_attention(q, bt.Kc, bt.Vc, bt.pages, bt.starts, bt.lens, D ** -0.5)
+    kmax = max(np.abs(A.gather(bt.Kc, bt.pages[b], t)).max() for b, t in enumerate(bt.lens))
+    check_close("O", I.to_host(out), O, attention_bound(O, M, q, kmax, D, D ** -0.5, bt.max_len, dtype))
