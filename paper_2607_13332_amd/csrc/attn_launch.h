@@ -78,6 +78,13 @@ struct AttnArgs {
 // `chunk`; where a sequence (rows kernel) or row tile (tile kernel) has more
 // than one, partial results are staged and joined: O unnormalized and (m, l)
 // of every row, range by range.
+//
+// Ranges that `keys` keys make, and the end of the one that begins at `begin`.
+// (Not by a sum of keys and chunk: lengths reach 2^31 - 4097.)
+__host__ __device__ inline int key_ranges(int keys, int chunk) { return keys > chunk ? (keys - 1) / chunk + 1 : 1; }
+__host__ __device__ inline int range_end(int begin, int chunk, int keys) {
+  return keys - begin < chunk ? keys : begin + chunk;
+}
 struct AttnPart {
   int blocks;           // 16-row blocks of a wave (0: kernel not launched)
   int chunk, ranges;    // keys of a range, ranges of the longest sequence

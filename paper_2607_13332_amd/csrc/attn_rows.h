@@ -34,11 +34,11 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, const AttnPart& pa
   const Sequence sq = sequence_of(a.pb, b);
   const int n = sq.s1 - sq.s0, rows = n * a.G, keys = sq.len;
   if (rows == 0 || rows > few) return;
-  const int ranges = keys > part.chunk ? (keys + part.chunk - 1) / part.chunk : 1;
+  const int ranges = key_ranges(keys, part.chunk);
   if (range >= ranges) return;
   const int bytes = a.D * (int)sizeof(T), before = sq.len - n;
   const int k_begin = range * part.chunk;
-  const int k_end = keys < k_begin + part.chunk ? keys : k_begin + part.chunk;
+  const int k_end = range_end(k_begin, part.chunk, keys);
 
   int row[QB], seen[QB];
   u32x4 qf[QB][NC];

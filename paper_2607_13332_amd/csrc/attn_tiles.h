@@ -214,7 +214,7 @@ __device__ __forceinline__ void tiles_block(const AttnArgs& a, const AttnPart& p
   const int before = sq.len - n;                           // position of the sequence's token 0
   const int last = r0 + BM < rows ? r0 + BM - 1 : rows - 1;
   const int keys = before + last / a.G + 1;                // that the tile sees
-  const int ranges = keys > part.chunk ? (keys + part.chunk - 1) / part.chunk : 1;
+  const int ranges = key_ranges(keys, part.chunk);
   if (range >= ranges) return;
 
   const int bytes = a.D * (int)sizeof(T);

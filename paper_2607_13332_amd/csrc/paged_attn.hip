@@ -93,7 +93,7 @@ __device__ __forceinline__ bool join_row(const AttnArgs& a, const AttnPart& p, i
     const int bm = 64 * p.blocks, last = (j.r / bm + 1) * bm - 1;
     keys = j.sq.len - n + (last < rows ? last : rows - 1) / a.G + 1;
   }
-  j.ranges = keys > p.chunk ? (keys + p.chunk - 1) / p.chunk : 1;
+  j.ranges = key_ranges(keys, p.chunk);
   return j.ranges > 1;
 }
 

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from attn_helpers import DEV, TORCH, Batch, attention_bound, check_close, dev
+from helpers import U_F32, ulp
 from oracle import attn_oracle as A
 from paper_2607_13332_amd import inputs as I
 from paper_2607_13332_amd import ssn
@@ -53,3 +54,33 @@ def test_two_staged_parts_with_an_odd_number_of_rows(dtype):
     O, _, M = A.paged_attention(q, bt.Kc, bt.Vc, bt.pages, bt.starts, bt.lens, D ** -0.5)
     kmax = max(np.abs(A.gather(bt.Kc, bt.pages[b], t)).max() for b, t in enumerate(bt.lens))
     check_close("O", I.to_host(out), O, attention_bound(O, M, q, kmax, D, D ** -0.5, bt.max_len, dtype))
+
+
+@pytest.mark.parametrize("new", [1, 33])
+def test_lengths_near_the_limit(new):
+    """2047 x 2^20 keys, every table entry the same page.  Keys are zero, so every
+    probability is one, and values are zeros and ones: the sums over one of 256
+    ranges (8.4 million keys) are whole numbers below 2^24, exact in float32.  Left
+    are 256 additions and multiplications of the join, a division, and of the
+    logarithm (21.5) some units of 2^-20."""
+    page, width, D = 2 ** 20, 2047, 8
+    length = width * page - 5
+    r = np.random.default_rng(3)
+    v = r.integers(0, 2, (page, D)).astype(np.float64)
+    cache = lambda a: dev(I.store(a[None, None], "bf16"), "bf16")  # noqa: E731
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+    ws = ssn.paged_attention_workspace(new, 1, 1, 1, D, new, length, DEV)
+    assert ws is not None
+    q = dev(I.store(r.standard_normal((new, 1, D)), "bf16"), "bf16")
+    out = torch.full((new, 1, D), 7e6, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((new, 1), 7e6, dtype=torch.float32, device=DEV)
+    print(f"[case] attention of {new} tokens over {length} keys", flush=True)
+    ssn.paged_attention(q, cache(np.zeros((page, D))), cache(v), torch.zeros((1, width), dtype=torch.int32, device=DEV),
+                        i32([0, new]), i32([length]), new, length, out=out, lse=lse, workspace=ws)
+    # position t is key t mod 2^20; token i sees length - new + i + 1 of them
+    seen = length - new + 1 + np.arange(new)
+    ones = seen[:, None] // page * v.sum(0) + np.stack([v[:n % page].sum(0) for n in seen])
+    ref = ones / seen[:, None]
+    join = 2 * 256 * U_F32
+    check_close("O", I.to_host(out)[:, 0], ref, ulp(ref, True) + join * ref)
+    check_close("lse", lse.cpu().numpy()[:, 0], np.log(seen), np.full(new, join + 2.0 ** -17))
