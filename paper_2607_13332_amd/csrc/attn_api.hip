@@ -13,8 +13,10 @@ namespace {
 
 constexpr int64_t kMaxElems = (int64_t)1 << 56;   // keeps every byte offset in int64
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 4096;   // rows of heads, cache rows, positions
-constexpr int64_t kMaxAttnRows = (int64_t)1 << 28;         // of attention: one grid holds its blocks
-constexpr int64_t kMaxAttnSeqs = (int64_t)1 << 22;         // sequences times key heads, the same
+// Of attention: one grid holds its blocks with one range of keys, and the plan
+// takes no more ranges than fit.
+constexpr int64_t kMaxAttnRows = (int64_t)1 << 28;
+constexpr int64_t kMaxAttnSeqs = (int64_t)1 << 22;         // sequences times key heads
 constexpr int64_t kMaxD = 1024;
 constexpr int64_t kMaxB = 1 << 20;
 

@@ -1,6 +1,7 @@
 // The paged attention's kernels: tiles, rows, or both in one launch.
 #pragma once
 
+#include "attn_plan.h"
 #include "attn_rows.h"
 #include "attn_tiles.h"
 
@@ -51,15 +52,15 @@ __global__ __launch_bounds__(256, (both_blocks<T, DT>())) void paged_attn_both(A
 
 template <typename T, int DT, int QB, bool EXACT>
 static hipError_t launch_rows(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
-  const int64_t grid = (int64_t)a.pb.B * a.Hk * p.rows.ranges;
-  hipLaunchKernelGGL((paged_attn_rows<T, DT, QB, EXACT>), dim3((unsigned)grid), dim3(256), 0, st, a, p.rows, p.few);
+  hipLaunchKernelGGL((paged_attn_rows<T, DT, QB, EXACT>), dim3((unsigned)row_blocks(p, a.pb.B, a.Hk)), dim3(256), 0,
+                     st, a, p.rows, p.few);
   return hipGetLastError();
 }
 template <typename T, int DT, int QB, bool EXACT>
 static hipError_t launch_tiles(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
-  const int64_t slots = tile_slots(a.pb.N, a.pb.B, a.G, 64 * QB), tiles = slots * a.Hk * p.tiles.ranges;
+  const int64_t slots = tile_slots(a.pb.N, a.pb.B, a.G, 64 * QB), tiles = tile_blocks(p, a.pb.N, a.pb.B, a.Hk, a.G);
   if (p.rows.blocks) {
-    const int64_t rows = (int64_t)a.pb.B * a.Hk * p.rows.ranges;
+    const int64_t rows = row_blocks(p, a.pb.B, a.Hk);
     hipLaunchKernelGGL((paged_attn_both<T, DT, QB, EXACT>), dim3((unsigned)(tiles + rows)), dim3(256), 0, st, a, p,
                        (int)slots, (int)rows);
   } else {

@@ -36,7 +36,6 @@ __device__ __forceinline__ void load_to_lds(const char* from, const char* to) {
 // sequence b has the numbers from starts[b] * G / BM + b on, which leaves ceil(rows
 // / BM) to each, some numbers name none, and the last goes first.
 constexpr int kCounted = 256;
-inline int64_t tile_slots(int64_t N, int64_t B, int64_t G, int64_t BM) { return N * G / BM + B; }
 __device__ __forceinline__ int first_slot(const PagedBatch& pb, int b, int G, int BM) {
   return (int)((int64_t)clampi(pb.starts[b], 0, pb.N) * G / BM) + b;
 }

@@ -84,3 +84,34 @@ def test_lengths_near_the_limit(new):
     join = 2 * 256 * U_F32
     check_close("O", I.to_host(out)[:, 0], ref, ulp(ref, True) + join * ref)
     check_close("lse", lse.cpu().numpy()[:, 0], np.log(seen), np.full(new, join + 2.0 ** -17))
+
+
+def test_many_sequences_without_new_tokens():
+    """200000 sequences of which four have new tokens, under bounds that allow
+    128 ranges of keys: more blocks than a launch holds, if every sequence had
+    them all."""
+    B, page, Hq, Hk, D, max_len = 200_000, 64, 4, 1, 64, 32768
+    few = Batch([(64, 9000), (1, 20000), (3, 3), (50, 700)], Hk, D, page, "bf16", 4, pad=2)
+    at = [0, 17, 123_456, B - 1]
+    pages = np.full((B, max_len // page), -1, np.int32)
+    lens = np.full(B, 5, np.int32)
+    new = np.zeros(B, np.int64)
+    for b, n in enumerate(at):
+        pages[n, :few.pages.shape[1]] = few.pages[b]
+        lens[n], new[n] = few.lens[b], few.new[b]
+    starts = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    r = np.random.default_rng(1)
+    q = I.store(1.5 * r.standard_normal((few.N, Hq, D)), "bf16")
+    Kc, Vc, *_ = few.device()
+    i32 = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    ws = ssn.paged_attention_workspace(few.N, B, Hq, Hk, D, few.max_q, max_len, DEV)
+    out = torch.full((few.N, Hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    print(f"[case] attention, {B} sequences", flush=True)
+    ssn.paged_attention(dev(q, "bf16"), Kc, Vc, i32(pages), i32(starts), i32(lens), few.max_q, max_len, out=out,
+                        workspace=ws)
+    O, _, M = A.paged_attention(q, few.Kc, few.Vc, few.pages, few.starts, few.lens, D ** -0.5)
+    kmax = max(np.abs(A.gather(few.Kc, few.pages[b], t)).max() for b, t in enumerate(few.lens))
+    bound = attention_bound(O, M, q, kmax, D, D ** -0.5, few.max_len, "bf16")
+    got, inside = I.to_host(out), slice(0, int(few.starts[-1]))
+    check_close("O", got[inside], O[inside], bound[inside])
+    assert (out[inside.stop:] == 7).all()
