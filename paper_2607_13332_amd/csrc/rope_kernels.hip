@@ -12,14 +12,13 @@
 
 namespace ssn {
 
-__global__ __launch_bounds__(256) void rope_table_kernel(float* __restrict__ table, int64_t P, int half,
+__global__ __launch_bounds__(256) void rope_table_kernel(float* __restrict__ table, int64_t P, int64_t half,
                                                          double log_theta) {
   const int64_t n = P * half;
   for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
-    const int64_t p = e / half;
-    const int i = (int)(e - p * half);
+    const int64_t p = e / half, i = e - p * half;
     double s, c;
-    sincos((double)p * exp(-log_theta * i / half), &s, &c);
+    sincos((double)p * exp(-log_theta * (double)i / (double)half), &s, &c);
     table[p * 2 * half + i] = (float)c;
     table[p * 2 * half + half + i] = (float)s;
   }
@@ -28,7 +27,7 @@ __global__ __launch_bounds__(256) void rope_table_kernel(float* __restrict__ tab
 hipError_t launch_rope_table(int64_t P, int64_t R, double theta, float* table, hipStream_t st) {
   const int64_t n = P * (R / 2), blocks = (n + 255) / 256;
   hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), 0, st,
-                     table, P, (int)(R / 2), log(theta));
+                     table, P, R / 2, log(theta));
   return hipGetLastError();
 }
 

@@ -115,3 +115,15 @@ def test_many_sequences_without_new_tokens():
     got, inside = I.to_host(out), slice(0, int(few.starts[-1]))
     check_close("O", got[inside], O[inside], bound[inside])
     assert (out[inside.stop:] == 7).all()
+
+
+def test_rope_table_past_32_bits():
+    """More than 2^31 pairs of a position (the table is 34 GB)."""
+    R, theta = 2 ** 32 + 2, 1e4
+    half = R // 2
+    out = torch.full((2, R), 7.0, dtype=torch.float32, device=DEV)
+    ssn.rope_table(2, R, theta, out=out)
+    for i in (0, 1, half // 2, 2 ** 31 - 1, half - 1):
+        a = theta ** (-2.0 * i / R)
+        got = out[:, [i, half + i]].double().cpu().numpy()
+        assert np.abs(got - [[1, 0], [np.cos(a), np.sin(a)]]).max() <= 2.0 ** -24 + 2.0 ** -50
