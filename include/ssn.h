@@ -586,10 +586,13 @@ ssn_status_t ssn_kv_append(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq, 
  *                   ssn_paged_attention_workspace_bytes is the size that
  *                   allows every split; a smaller one (or NULL with 0 bytes)
  *                   allows fewer or none.
- * Products of bf16 storage are matrix-core products with float32 sums; the
- * probabilities are rounded to bf16 for the product with V, their sum is not.
- * Float32 storage is computed in float32 throughout.  Repeated calls give the
- * same bits.
+ * Products of bf16 storage are matrix-core products with float32 sums.  For the
+ * product with V the probabilities are rounded to bf16 (2^-8 of each at most)
+ * where a sequence has many rows (new tokens times the heads of a group), and
+ * held to 2^-16 where it has few: in batches of up to 32 rows a sequence (16
+ * above D = 128), and for sequences of up to 16 among longer chunks.  Their sum
+ * is not rounded.  Float32 storage is computed in float32 throughout.  Repeated
+ * calls give the same bits.
  */
 size_t ssn_paged_attention_workspace_bytes(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq,
                                            int64_t Hk, int64_t D, int64_t max_q, int64_t max_len);

@@ -10,7 +10,7 @@ namespace ssn {
 // Blocks of a compute unit: two where 256 registers hold a wave's rows (and, in
 // the rows kernel, its keys and values: float32, 16 single tokens over up to 8192
 // keys, 8 heads of 128: 128 us with two, 155 with one; bf16 rows of 32 or heads
-// of 256 spill with two: 118 us become 190, 87 become 140).
+// of 256 spill with two: 118 us became 190, 87 became 140, with probabilities in one part).
 template <typename T, int DT, int QB>
 constexpr int rows_blocks() { return DT * (int)sizeof(T) * QB <= (sizeof(T) == 4 ? 512 : 256) ? 2 : 1; }
 template <typename T, int DT>

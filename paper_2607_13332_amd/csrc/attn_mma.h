@@ -46,11 +46,21 @@ struct Mma<uint16_t> {
   static constexpr int kKeys = 32;         // keys of one step of the second product
   __device__ static __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) { return mfma16x16x32(a, b, c); }
   // Probabilities of a step from its tiles of S^T, rounded to bf16 (nearest
-  // even): 2^-9 of each at most, next to the 2^-9 of the rounded output.
+  // even): off by 2^-8 of each at most, as the rounded output is.
   __device__ static __forceinline__ u32x4 probs(const f32x4* s) {
     return u32x4{pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]), pack_bf16x2(s[1][0], s[1][1]),
                  pack_bf16x2(s[1][2], s[1][3])};
   }
+  // What that rounding left, rounded in turn: with both a probability is off by
+  // 2^-16 at most, and its product with V is a float32 one for all that shows.
+  __device__ static __forceinline__ u32x4 remainders(const f32x4* s, u32x4 p) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      r[i] = pack_bf16x2(s[i >> 1][2 * (i & 1)] - lo_bf16(p[i]), s[i >> 1][2 * (i & 1) + 1] - hi_bf16(p[i]));
+    return r;
+  }
+  static constexpr int kParts = 2;         // of a probability, where a kernel takes them
   static constexpr int kTiles = 2;         // tiles of S^T in a step
   // V^T of 16 d's for a step: lane's d = 16 dt + lane % 16, its keys 4 (lane /
   // 16) + i of the step's two tiles.  `vb`: vbase() of the lane.
@@ -65,6 +75,19 @@ struct Mma<uint16_t> {
     const char* p = lds + (vb[0] ^ (uint32_t)(dt * 32)) + step * 32 * RB;
     const u32x2 a = lds_read_tr16((const uint16_t*)p), b = lds_read_tr16((const uint16_t*)(p + 16 * RB));
     return u32x4{a[0], a[1], b[0], b[1]};
+  }
+  // v with infinities and NaN as the largest numbers of their sign: as unsigned
+  // numbers they are the largest of the negative ones, as signed of the others.
+  __device__ static __forceinline__ u32x4 bounded(u32x4 v) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = v[i];         // (a bit cast of the element itself takes the first one)
+      const u16x2 n = __builtin_elementwise_min(__builtin_bit_cast(u16x2, w), u16x2{0xFF7F, 0xFF7F});
+      v[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(i16x2, n), i16x2{0x7F7F, 0x7F7F}));
+    }
+    return v;
   }
   // v with infinities and NaN as zeros.
   __device__ static __forceinline__ u32x4 finite_part(u32x4 v) {
@@ -87,6 +110,7 @@ struct Mma<float> {
     return c;
   }
   __device__ static __forceinline__ u32x4 probs(const f32x4* s) { return __builtin_bit_cast(u32x4, s[0]); }
+  static constexpr int kParts = 1;
   static constexpr int kTiles = 1;
   template <int RB>
   __device__ static __forceinline__ uint32_t vbase(int lane, int i) {
@@ -134,9 +158,10 @@ struct RowState {
 // maximum is taken otherwise.  Rows do not touch each other's bits.
 constexpr float kFar = 1024.f;
 __device__ __forceinline__ bool far(float sum, float m) { return !(sum <= kFar) || m == kNegInf; }
-template <typename T, int NKB, int QB>
+// PARTS of a probability: it as it is rounded, then what the rounding left.
+template <typename T, int PARTS, int NKB, int QB>
 __device__ __forceinline__ bool probabilities(const f32x4 (&s)[NKB][QB], const float (&m)[QB], float c,
-                                              u32x4 (&p)[NKB / Mma<T>::kTiles][QB], float (&sum)[QB]) {
+                                              u32x4 (&p)[PARTS][NKB / Mma<T>::kTiles][QB], float (&sum)[QB]) {
   using M = Mma<T>;
   bool any = false;
 #pragma unroll
@@ -154,17 +179,18 @@ __device__ __forceinline__ bool probabilities(const f32x4 (&s)[NKB][QB], const f
           x[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t * M::kTiles + u][q][i], c, -base));
           sum[q] += x[u][i];
         }
-      p[t][q] = M::probs(x);
+      p[0][t][q] = M::probs(x);
+      if constexpr (PARTS == 2) p[1][t][q] = M::remainders(x, p[0][t][q]);
     }
     any |= far(sum[q], m[q]);
   }
   return any;
 }
-template <typename T, int NKB, int DT16, int QB>
+template <typename T, int PARTS, int NKB, int DT16, int QB>
 __device__ __forceinline__ void softmax_step(const f32x4 (&s)[NKB][QB], RowState<DT16, QB>& st, float c,
-                                             u32x4 (&p)[NKB / Mma<T>::kTiles][QB]) {
+                                             u32x4 (&p)[PARTS][NKB / Mma<T>::kTiles][QB]) {
   float sum[QB];
-  if (__any(probabilities<T>(s, st.m, c, p, sum))) {
+  if (__any(probabilities<T, PARTS>(s, st.m, c, p, sum))) {
 #pragma unroll
     for (int q = 0; q < QB; ++q) {
       int move = far(sum[q], st.m[q]);
@@ -184,7 +210,7 @@ __device__ __forceinline__ void softmax_step(const f32x4 (&s)[NKB][QB], RowState
 #pragma unroll
       for (int d = 0; d < DT16; ++d) st.o[d][q] *= fade;
     }
-    probabilities<T>(s, st.m, c, p, sum);
+    probabilities<T, PARTS>(s, st.m, c, p, sum);
   }
 #pragma unroll
   for (int q = 0; q < QB; ++q) st.l[q] += sum[q];
@@ -193,8 +219,8 @@ __device__ __forceinline__ void softmax_step(const f32x4 (&s)[NKB][QB], RowState
 // O^T += V^T P^T over NS steps of keys in LDS.  MASKED: some rows do not
 // see some of its keys, and 0 times an infinity or a NaN there would reach
 // them; what is not finite is left out (`odd` says so) for add_not_finite().
-template <typename T, int RB, bool MASKED, int NS, int DT16, int QB>
-__device__ __forceinline__ void weigh(const char* vlds, const uint32_t* vb, const u32x4 (&p)[NS][QB],
+template <typename T, int RB, bool MASKED, int PARTS, int NS, int DT16, int QB>
+__device__ __forceinline__ void weigh(const char* vlds, const uint32_t* vb, const u32x4 (&p)[PARTS][NS][QB],
                                       RowState<DT16, QB>& st, uint32_t& odd) {
   using M = Mma<T>;
 #pragma unroll
@@ -207,8 +233,15 @@ __device__ __forceinline__ void weigh(const char* vlds, const uint32_t* vb, cons
         odd |= (f[0] ^ v[0]) | (f[1] ^ v[1]) | (f[2] ^ v[2]) | (f[3] ^ v[3]);
         v = f;
       }
+      if constexpr (PARTS == 2) {
+        // (a remainder may be zero or negative: an infinity times it would be NaN
+        // or of the other sign)
+        const u32x4 f = MASKED ? v : M::bounded(v);
 #pragma unroll
-      for (int q = 0; q < QB; ++q) st.o[d][q] = M::mma(v, p[t][q], st.o[d][q]);
+        for (int q = 0; q < QB; ++q) st.o[d][q] = M::mma(f, p[1][t][q], st.o[d][q]);
+      }
+#pragma unroll
+      for (int q = 0; q < QB; ++q) st.o[d][q] = M::mma(v, p[0][t][q], st.o[d][q]);
     }
   }
 }

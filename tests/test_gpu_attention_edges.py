@@ -127,3 +127,66 @@ def test_rope_table_past_32_bits():
         a = theta ** (-2.0 * i / R)
         got = out[:, [i, half + i]].double().cpu().numpy()
         assert np.abs(got - [[1, 0], [np.cos(a), np.sin(a)]]).max() <= 2.0 ** -24 + 2.0 ** -50
+
+
+@pytest.mark.parametrize("new", [1, 5])
+@pytest.mark.parametrize("D", [64, 128, 256, 80])
+@pytest.mark.parametrize("visible", [0, 500])
+def test_probabilities_of_few_rows_keep_their_bits(D, new, visible):
+    """bf16 rows of up to 32 of a key head: probabilities near each other under
+    values of +-1, so that what is left of their sum is a few hundredths and a
+    rounding of the probabilities to bf16 (2^-8 each) would show.
+
+    Scores are single products (a query is a unit vector), exact in float32.  Left
+    are 2^-16 of a probability (two bf16 parts), the exponential's 2^-20, sums of
+    at most 14 terms that are not zero, and the output's rounding."""
+    Hq, Hk = (6, 2) if new == 1 else (10, 2)
+    if D == 256 and new > 1:
+        Hq = 6
+    seqs = [(new, visible + n) for n in (5, 6, 7, 9, 13, 14)]
+    bt = Batch(seqs, Hk, D, 16, "bf16", 7)
+    r = np.random.default_rng(D + new)
+    for b, (_, length) in enumerate(seqs):
+        page, off = bt.slots(b)
+        # the first `visible` keys have no weight, the others almost the same
+        x = np.zeros((length, Hk, D))
+        x[:, :, 0] = np.where(np.arange(length)[:, None] < visible, -200.0, r.uniform(-0.2, 0.2, (length, Hk)))
+        bt.Kc[page, :, off] = I.store(x, "bf16")
+        v = np.where((np.arange(length)[:, None, None] + np.arange(D)) % 2, 1.0, -1.0) * np.ones((1, Hk, 1))
+        bt.Vc[page, :, off] = I.store(v, "bf16")
+    q = np.zeros((bt.N, Hq, D))
+    q[:, :, 0] = 1.0
+    q = I.store(q, "bf16")
+    Kc, Vc, pages, starts, lens = bt.device()
+    ws = ssn.paged_attention_workspace(bt.N, len(seqs), Hq, Hk, D, new, bt.max_len, DEV)
+    for w in (ws, None):
+        out = ssn.paged_attention(dev(q, "bf16"), Kc, Vc, pages, starts, lens, new, bt.max_len, scale=1.0, workspace=w)
+        O, _, M = A.paged_attention(q, bt.Kc, bt.Vc, bt.pages, bt.starts, bt.lens, 1.0)
+        assert np.abs(O).min() < 0.05
+        check_close("O", I.to_host(out), O, ulp(O, True) + (2.0 ** -16 + 2.0 ** -20 + 32 * U_F32) * M)
+
+
+@pytest.mark.parametrize("new", [1, 4])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("equal", [True, False])
+def test_infinite_values_that_few_rows_see(D, new, equal):
+    """An infinite value, positive or negative, in a tile that every row sees
+    reaches its element with its sign, a NaN as one, and no other element."""
+    Hq, Hk, length = 4, 2, 600
+    bt = Batch([(new, length)], Hk, D, 16, "bf16", 3)
+    r = np.random.default_rng(2)
+    q = dev(I.store((0.0 if equal else 1.5) * r.standard_normal((new, Hq, D)), "bf16"), "bf16")
+    Kc, Vc, pages, starts, lens = bt.device()
+    ws = ssn.paged_attention_workspace(new, 1, Hq, Hk, D, new, length, DEV)
+    for w in (ws, None):
+        args = (pages, starts, lens, new, length)
+        clean = ssn.paged_attention(q, Kc, Vc, *args, workspace=w).float()
+        page, off = bt.slots(0)
+        bad = Vc.clone()
+        for t, e, x in [(3, 7, float("inf")), (40, 20, -float("inf")), (333, 40, float("nan")), (100, 41, 3e38)]:
+            bad[int(page[t]), :, int(off[t]), e] = x
+        got = ssn.paged_attention(q, Kc, bad, *args, workspace=w).float()
+        assert (got[..., 7] == float("inf")).all() and (got[..., 20] == -float("inf")).all()
+        assert torch.isnan(got[..., 40]).all() and torch.isfinite(got[..., 41]).all()
+        keep = [e for e in range(D) if e not in (7, 20, 40, 41)]
+        assert torch.equal(got[..., keep], clean[..., keep])
