@@ -577,7 +577,8 @@ ssn_status_t ssn_kv_append(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq, 
  * written.  What the cache holds in positions a row does not see has no
  * effect on it, whatever it is.
  *   max_q, max_len  host bounds on a sequence's new tokens and length; they
- *                   choose the launch shape
+ *                   choose the launch shape, and loose ones cost time (few
+ *                   tokens over 8192 keys: 4 times under a bound of 131072)
  *   O [N, Hq, D] dtype;  lse [N, Hq] float32 or NULL: the natural logarithm of
  *                   sum_t exp(scale Q . K_t)
  *   workspace       16-byte aligned device memory, any contents: where rows

@@ -4,10 +4,10 @@
 // results in LDS at the end.
 //
 // What bounds it: reading the cache.  64 single tokens over caches of 1 to 4096
-// keys (40 / 8 heads of 128, bf16) take 98 us (5.6 TB/s), four over 100000 to
-// 131072 keys 314 us (6.7 TB/s; a large copy moves 4.6), and the join 7 to 9 us
+// keys (40 / 8 heads of 128, bf16) take 100 us (5.5 TB/s), four over 100000 to
+// 131072 keys 316 us (6.7 TB/s; a large copy moves 4.6), and the join 7 to 10 us
 // more.  The matrix cores are used with 16 rows where a group has 4 or 5 heads:
-// they are busy 4 % of the time, and each key is read once for the group.
+// they are busy 6 % of the time, and each key is read once for the group.
 //
 // bf16 probabilities are multiplied in two parts (their rounding and what it left),
 // which the matrix cores have room for: single tokens with heads of 64 and 128 take

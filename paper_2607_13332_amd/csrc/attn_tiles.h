@@ -36,9 +36,10 @@ __device__ __forceinline__ void load_to_lds(const char* from, const char* to) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(at) : "memory");
 }
 
-// The launch's row tiles, those that see the most keys first: a sequence's last
-// tile sees the most.  Up to kCounted sequences every block counts the tiles of
-// each (four a lane) and ranks them by their place in their sequence; past that
+// The launch's row tiles by their place in their sequence, the last places first:
+// of prompts without cached keys before them, those that see the most keys.  (What
+// is cached before a chunk is not looked at.)  Up to kCounted sequences every block
+// counts the tiles of each (four a lane) and ranks them over all; past that
 // sequence b has the numbers from starts[b] * G / BM + b on, which leaves ceil(rows
 // / BM) to each, some numbers name none, and the last goes first.
 constexpr int kCounted = 256;

@@ -1,9 +1,10 @@
-// Attention of new tokens over a paged cache: dispatch and the generic kernel.
+// Attention of new tokens over a paged cache: dispatch, the join of ranges and the
+// generic kernel (the matrix-core kernels: attn_tiles.h, attn_rows.h).
 //
 //   O_i = sum_{t <= p_i} softmax_t(scale q_i . k_t) v_t
 //
-// in one pass over the keys with the running maximum m and sum l of the
-// softmax: for a tile of scores s, m' = max(m, max s), and with a =
+// The generic kernel makes one pass over the keys with the running maximum m and
+// sum l of the softmax: for a tile of scores s, m' = max(m, max s), and with a =
 // exp(m - m'), l' = a l + sum exp(s - m'), O' = a O + sum exp(s - m') v; at
 // the end O / l.
 #include "attn_mma.h"

@@ -845,7 +845,7 @@ def paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, pages: 
     """Attention of new tokens Q [N, Hq, D] over the paged cache that holds
     their keys and values already: each sees its sequence up to itself.  max_q
     and max_len bound the new tokens and the length of a sequence (host
-    numbers); scale defaults to D^-1/2; lse [N, Hq] float32 receives the
+    numbers; the launch shape follows them, so near ones are faster); scale defaults to D^-1/2; lse [N, Hq] float32 receives the
     logarithms of the softmax sums.  Without a workspace (1-D uint8, from
     paged_attention_workspace()) the keys are not split."""
     N, Hq, D = Q.shape
