@@ -24,9 +24,9 @@ inline size_t stage_bytes(const AttnPart& p, int64_t D) {
   return ((size_t)p.ranges * (size_t)p.stage_rows * (size_t)(D + 2) * 4 + 15) / 16 * 16;
 }
 // Ranges for about `want` of them, no more than `fit` bytes hold.  They divide
-// max_len: 512 tokens over 32768 keys take 366 us under that bound and 964 under
-// 131072 (64 over 8192: 36 and 130), 64 single tokens over caches of 1 to 4096 keys 108 and 129, one over 2011
-// keys 14 and 33.
+// max_len: under their own bound and under 131072, us, 512 tokens over 32768 keys
+// take 366 and 964, 64 over 8192 36 and 130, 64 single tokens over caches of 1 to
+// 4096 keys 108 and 129, one over 2011 keys 14 and 33.
 inline void split_keys(AttnPart& p, int64_t want, int64_t unit, int64_t max_len, int64_t D, size_t fit) {
   const int64_t row_bytes = p.stage_rows * (D + 2) * 4;
   if (row_bytes > 0 && (size_t)want > fit / (size_t)row_bytes) want = (int64_t)(fit / (size_t)row_bytes);
