@@ -605,6 +605,72 @@ ssn_status_t ssn_paged_attention(ssn_dtype_t dtype, int64_t N, int64_t B, int64_
                                  int64_t ldo, float *lse, void *workspace, size_t workspace_bytes,
                                  void *stream);
 
+/*
+ * The same cache in 4 bits an element (4.25 with its scales, 17 / 64 of bf16's
+ * bytes).  A cache of keys or of values is two byte arrays on the device,
+ *   codes  [npages, Hk, page_size, D / 2]   two elements a byte, the first in
+ *                                           the low half
+ *   scales [npages, Hk, page_size, D / 32]  one for 32 consecutive elements
+ * and D is a multiple of 32 (else SSN_ERR_SHAPE), at most 1024
+ * (SSN_ERR_UNSUPPORTED).  A scale byte s below 255 stands for 2^(s - 127), a
+ * code's bit 3 for the sign and its lower bits for 0, 0.5, 1, 1.5, 2, 3, 4, 6;
+ * under s = 255 all 32 elements are NaN.  Any bytes are a valid cache.  Sizes,
+ * batches, rows of heads and what is clamped are those of the cache above.  The
+ * fast paths need 16-byte aligned codes and, in the attention, D <= 256; no
+ * alignment is asked of codes and scales.
+ */
+
+/*
+ * ssn_kv_append_fp4 -- ssn_kv_append into a 4-bit cache: keys (normed and
+ * rotated) and values of a batch's new tokens to their slots, queries to Qout.  A
+ * group is written with the smallest e, -126 <= e <= 125, for which its largest
+ * magnitude is below 7 2^e and so rounds to 6 2^e at most; s = e + 127, and every
+ * element becomes the nearest level times 2^e, ties to the even code, magnitudes
+ * past 6 2^125 becoming that.  Keys are rounded once, from float32.  A group that
+ * holds an infinity or a NaN gets s = 255 and codes of zero.  No two rows may
+ * share a cache slot.
+ */
+ssn_status_t ssn_kv_append_fp4(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk,
+                               int64_t D, int64_t R, int64_t P, ssn_rope_t style, float eps,
+                               const void *Q, int64_t ldq, const void *K, int64_t ldk,
+                               const void *V, int64_t ldv, const void *wq, const void *wk,
+                               const float *table, uint8_t *Kc, uint8_t *Ks, uint8_t *Vc,
+                               uint8_t *Vs, int64_t npages, int64_t page_size,
+                               const int32_t *pages, int64_t width, const int32_t *starts,
+                               const int32_t *lens, void *Qout, int64_t ldqo, void *stream);
+
+/*
+ * ssn_kv_read_fp4 -- the way back: row i of K and V [N, Hk, D] (outputs, dtype)
+ * becomes what the cache holds at the row's position, sequence b's rows being its
+ * last starts[b + 1] - starts[b] positions (all of them, if that is its length).
+ * Exact in both types, but for what is past bf16's range (s of 253 and 254 reach
+ * infinity).  Rows with a negative position and padding are not written.
+ */
+ssn_status_t ssn_kv_read_fp4(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hk, int64_t D,
+                             const uint8_t *Kc, const uint8_t *Ks, const uint8_t *Vc,
+                             const uint8_t *Vs, int64_t npages, int64_t page_size,
+                             const int32_t *pages, int64_t width, const int32_t *starts,
+                             const int32_t *lens, void *K, int64_t ldk, void *V, int64_t ldv,
+                             void *stream);
+
+/*
+ * ssn_paged_attention_fp4 -- ssn_paged_attention over a 4-bit cache, with K_t and
+ * V_t the values that it stands for (they are exact in bf16, so keys and values
+ * are not rounded again).  dtype is that of Q and O; the other arguments, the
+ * rounding of probabilities in bf16 and what a row does not see are as there.
+ */
+size_t ssn_paged_attention_fp4_workspace_bytes(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq,
+                                               int64_t Hk, int64_t D, int64_t max_q,
+                                               int64_t max_len);
+ssn_status_t ssn_paged_attention_fp4(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq,
+                                     int64_t Hk, int64_t D, int64_t max_q, int64_t max_len,
+                                     float scale, const void *Q, int64_t ldq, const uint8_t *Kc,
+                                     const uint8_t *Ks, const uint8_t *Vc, const uint8_t *Vs,
+                                     int64_t npages, int64_t page_size, const int32_t *pages,
+                                     int64_t width, const int32_t *starts, const int32_t *lens,
+                                     void *O, int64_t ldo, float *lse, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

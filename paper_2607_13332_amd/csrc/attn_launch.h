@@ -103,6 +103,8 @@ hipError_t launch_attn_rows_bf16(const AttnArgs& a, const AttnPlan& p, hipStream
 hipError_t launch_attn_rows_f32(const AttnArgs& a, const AttnPlan& p, hipStream_t st);
 hipError_t launch_attn_tiles_bf16(const AttnArgs& a, const AttnPlan& p, hipStream_t st);
 hipError_t launch_attn_tiles_f32(const AttnArgs& a, const AttnPlan& p, hipStream_t st);
+// Joins the partial results of a plan with more than one range.
+hipError_t launch_attn_join(int dtype, const AttnArgs& a, const AttnPlan& p, hipStream_t st);
 hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
 
 }  // namespace ssn

@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256) void paged_attn_join(AttnArgs a, AttnPlan plan
   }
 }
 
-static hipError_t launch_join(int dtype, const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
+hipError_t launch_attn_join(int dtype, const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   JoinShape js;
   js.lanes = 1;
   while (js.lanes * 4 < a.D) js.lanes *= 2;
@@ -237,7 +237,7 @@ hipError_t launch_paged_attention(int dtype, const AttnArgs& a, void* ws, size_t
   hipError_t e;
   if (p.tiles.blocks) e = dtype == kBF16 ? launch_attn_tiles_bf16(a, p, st) : launch_attn_tiles_f32(a, p, st);
   else e = dtype == kBF16 ? launch_attn_rows_bf16(a, p, st) : launch_attn_rows_f32(a, p, st);
-  return e == hipSuccess ? launch_join(dtype, a, p, st) : e;
+  return e == hipSuccess ? launch_attn_join(dtype, a, p, st) : e;
 }
 
 }  // namespace ssn

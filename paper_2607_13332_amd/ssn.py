@@ -130,6 +130,17 @@ def _declare(lib):
     lib.ssn_paged_attention.restype = ctypes.c_int
     lib.ssn_paged_attention.argtypes = [ctypes.c_int] + [_c_i64] * 7 + [ctypes.c_float, _c_p, _c_i64] + \
         paged + [_c_p, _c_i64, _c_p, _c_p, _sz, _c_p]
+    paged4 = [_c_p] * 4 + paged[2:]                                              # Kc, Ks, Vc, Vs .. lens
+    lib.ssn_kv_append_fp4.restype = ctypes.c_int
+    lib.ssn_kv_append_fp4.argtypes = [ctypes.c_int] + [_c_i64] * 7 + [ctypes.c_int, ctypes.c_float] + \
+        [_c_p, _c_i64] * 3 + [_c_p] * 3 + paged4 + [_c_p, _c_i64, _c_p]
+    lib.ssn_kv_read_fp4.restype = ctypes.c_int
+    lib.ssn_kv_read_fp4.argtypes = [ctypes.c_int] + [_c_i64] * 4 + paged4 + [_c_p, _c_i64] * 2 + [_c_p]
+    lib.ssn_paged_attention_fp4_workspace_bytes.restype = _sz
+    lib.ssn_paged_attention_fp4_workspace_bytes.argtypes = [ctypes.c_int] + [_c_i64] * 7
+    lib.ssn_paged_attention_fp4.restype = ctypes.c_int
+    lib.ssn_paged_attention_fp4.argtypes = [ctypes.c_int] + [_c_i64] * 7 + [ctypes.c_float, _c_p, _c_i64] + \
+        paged4 + [_c_p, _c_i64, _c_p, _c_p, _sz, _c_p]
     return lib
 
 
@@ -857,6 +868,133 @@ def paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, pages: 
         raise ValueError(f"lse has shape {tuple(lse.shape)}, expected ({N}, {Hq})")
     B, paged = _paged(Kc, Vc, pages, starts, lens, Q, g, t, Hk, D)
     _check("ssn_paged_attention", lib().ssn_paged_attention(
+        _code(t), N, B, Hq, Hk, D, max_q, max_len, D ** -0.5 if scale is None else float(scale),
+        *_rows(Q, "Q", Q, g, t, N, Hq, D), *paged, *_rows(out, "out", Q, g, t, N, Hq, D),
+        None if lse is None else _gpu(lse, "lse", Q, g, torch.float32, 2),
+        None if workspace is None else _gpu(workspace, "workspace", Q, g, torch.uint8, 1),
+        0 if workspace is None else workspace.numel(), _stream(stream)))
+    return out
+
+
+# --------------------------------------------------------------------------
+# The cache in 4 bits an element: codes [pages, Hk, page_size, D / 2] and scales
+# [pages, Hk, page_size, D / 32], uint8, for keys and for values; D a multiple
+# of 32.  32 consecutive elements share a power of two 2^(s - 127) and each is the
+# nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it, with its sign.
+# --------------------------------------------------------------------------
+FP4_GROUP = 32
+
+
+def fp4_cache(npages: int, Hk: int, page_size: int, D: int, device) -> tuple:
+    """(codes, scales) of a 4-bit cache of keys or of values: zeros, until
+    kv_append_fp4 fills them."""
+    if D % FP4_GROUP:
+        raise ValueError(f"heads of {D} elements: a 4-bit cache takes multiples of {FP4_GROUP}")
+    return (torch.zeros((npages, Hk, page_size, D // 2), dtype=torch.uint8, device=device),
+            torch.zeros((npages, Hk, page_size, D // FP4_GROUP), dtype=torch.uint8, device=device))
+
+
+def _paged_fp4(Kc, Ks, Vc, Vs, pages, starts, lens, first, g, Hk, D):
+    """(B, C arguments) of a batch of sequences over the 4-bit cache."""
+    kc = Kc.shape
+    if len(kc) != 4 or D % FP4_GROUP or kc[1] != Hk or kc[3] != D // 2 or Vc.shape != kc or \
+            Ks.shape != (*kc[:3], D // FP4_GROUP) or Vs.shape != Ks.shape:
+        raise ValueError(f"shape mismatch Kc{tuple(kc)} Ks{tuple(Ks.shape)} Vc{tuple(Vc.shape)} Vs{tuple(Vs.shape)}, "
+                         f"expected codes (pages, {Hk}, page_size, {D} / 2) and scales "
+                         f"(pages, {Hk}, page_size, {D} / {FP4_GROUP})")
+    if pages.dim() != 2:
+        raise ValueError(f"pages must be [B, width], got {tuple(pages.shape)}")
+    B, width = pages.shape
+    if starts.numel() != B + 1 or lens.numel() != B:
+        raise ValueError(f"shape mismatch pages{tuple(pages.shape)} starts{tuple(starts.shape)} "
+                         f"lens{tuple(lens.shape)}")
+    u8, i32 = torch.uint8, torch.int32
+    return B, (_gpu(Kc, "Kc", first, g, u8, 4), _gpu(Ks, "Ks", first, g, u8, 4), _gpu(Vc, "Vc", first, g, u8, 4),
+               _gpu(Vs, "Vs", first, g, u8, 4), kc[0], kc[2], _gpu(pages, "pages", first, g, i32, 2), width,
+               _gpu(starts, "starts", first, g, i32, 1), _gpu(lens, "lens", first, g, i32, 1))
+
+
+def kv_append_fp4(K: torch.Tensor, V: torch.Tensor, Kc: torch.Tensor, Ks: torch.Tensor, Vc: torch.Tensor,
+                  Vs: torch.Tensor, pages: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor,
+                  Q: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
+                  wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
+                  eps: Optional[float] = 1e-6, style: str = "halves",
+                  Qout: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """kv_append into a 4-bit cache, in place: keys [N, Hk, D], normed and rotated
+    to their positions (eps None: no norm; table None: no rotation), and values
+    are quantised on their way to their slots.  A group of 32 elements with an
+    infinity or a NaN reads back as NaN.  Returns Qout (None without Q)."""
+    N, Hk, D = K.shape
+    P, R, code, e = _rotation(table, style, eps, D, wq, wk)
+    t, g = K.dtype, K.get_device()
+    Hq, q, qo = 0, (None, 0), (None, 0)
+    if Q is not None:
+        Hq = Q.shape[1]
+        if Qout is None:
+            Qout = torch.empty((N, Hq, D), dtype=t, device=K.device)
+        q = _rows(Q, "Q", K, g, t, N, Hq, D)
+        qo = _rows(Qout, "Qout", K, g, t, N, Hq, D)
+    B, paged = _paged_fp4(Kc, Ks, Vc, Vs, pages, starts, lens, K, g, Hk, D)
+    _check("ssn_kv_append_fp4", lib().ssn_kv_append_fp4(
+        _code(t), N, B, Hq, Hk, D, R, P, code, e, *q, *_rows(K, "K", K, g, t, N, Hk, D),
+        *_rows(V, "V", K, g, t, N, Hk, D), _weight(wq, "wq", K, g, t, D) if Hq else None,
+        _weight(wk, "wk", K, g, t, D), _gpu(table, "table", K, g, torch.float32, 2) if R else None,
+        *paged, *qo, _stream(stream)))
+    return Qout if Q is not None else None
+
+
+def kv_read_fp4(Kc: torch.Tensor, Ks: torch.Tensor, Vc: torch.Tensor, Vs: torch.Tensor, pages: torch.Tensor,
+                starts: torch.Tensor, lens: torch.Tensor, N: int, dtype: torch.dtype = torch.bfloat16,
+                Kout: Optional[torch.Tensor] = None, Vout: Optional[torch.Tensor] = None, stream=None):
+    """What a 4-bit cache holds for the N rows of a batch, as kv_append_fp4 takes
+    them: (K, V) [N, Hk, D], sequence b's rows starts[b] .. starts[b + 1] - 1 its
+    last positions.  Rows of no sequence are not written."""
+    if Kc.dim() != 4:
+        raise ValueError(f"Kc must be [pages, Hk, page_size, D / 2], got {tuple(Kc.shape)}")
+    Hk, D, g = Kc.shape[1], 2 * Kc.shape[3], Kc.get_device()
+    if Kout is not None or Vout is not None:
+        dtype = (Vout if Kout is None else Kout).dtype
+    if Kout is None:
+        Kout = torch.empty((N, Hk, D), dtype=dtype, device=Kc.device)
+    if Vout is None:
+        Vout = torch.empty((N, Hk, D), dtype=dtype, device=Kc.device)
+    B, paged = _paged_fp4(Kc, Ks, Vc, Vs, pages, starts, lens, Kc, g, Hk, D)
+    _check("ssn_kv_read_fp4", lib().ssn_kv_read_fp4(
+        _code(dtype), N, B, Hk, D, *paged, *_rows(Kout, "Kout", Kc, g, dtype, N, Hk, D),
+        *_rows(Vout, "Vout", Kc, g, dtype, N, Hk, D), _stream(stream)))
+    return Kout, Vout
+
+
+def paged_attention_fp4_workspace_bytes(N: int, B: int, Hq: int, Hk: int, D: int, max_q: int, max_len: int,
+                                        dtype: torch.dtype = torch.bfloat16) -> int:
+    return int(lib().ssn_paged_attention_fp4_workspace_bytes(_dt_code(dtype), N, B, Hq, Hk, D, max_q, max_len))
+
+
+def paged_attention_fp4_workspace(N: int, B: int, Hq: int, Hk: int, D: int, max_q: int, max_len: int, device,
+                                  dtype: torch.dtype = torch.bfloat16) -> Optional[torch.Tensor]:
+    """A workspace for paged_attention_fp4 at this shape (None when it takes no
+    split); calls that share it must not overlap."""
+    n = paged_attention_fp4_workspace_bytes(N, B, Hq, Hk, D, max_q, max_len, dtype)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n > 0 else None
+
+
+def paged_attention_fp4(Q: torch.Tensor, Kc: torch.Tensor, Ks: torch.Tensor, Vc: torch.Tensor,
+                        Vs: torch.Tensor, pages: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor,
+                        max_q: int, max_len: int, scale: Optional[float] = None,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """paged_attention over a 4-bit cache: the new tokens Q [N, Hq, D] (bf16 or
+    float32) attend to the values that the cache stands for, theirs among them.
+    The other arguments are paged_attention's."""
+    N, Hq, D = Q.shape
+    Hk = Kc.shape[1] if Kc.dim() == 4 else 0
+    t, g = Q.dtype, Q.get_device()
+    if out is None:
+        out = torch.empty((N, Hq, D), dtype=t, device=Q.device)
+    if lse is not None and lse.shape != (N, Hq):
+        raise ValueError(f"lse has shape {tuple(lse.shape)}, expected ({N}, {Hq})")
+    B, paged = _paged_fp4(Kc, Ks, Vc, Vs, pages, starts, lens, Q, g, Hk, D)
+    _check("ssn_paged_attention_fp4", lib().ssn_paged_attention_fp4(
         _code(t), N, B, Hq, Hk, D, max_q, max_len, D ** -0.5 if scale is None else float(scale),
         *_rows(Q, "Q", Q, g, t, N, Hq, D), *paged, *_rows(out, "out", Q, g, t, N, Hq, D),
         None if lse is None else _gpu(lse, "lse", Q, g, torch.float32, 2),

@@ -1,0 +1,329 @@
+"""Appends to the 4-bit cache and reading it back, on the GPU against the oracle:
+codes and scales bit for bit where the inputs are quantised as they are, and
+between the roundings of the error bound's ends where a norm and a rotation come
+before."""
+import numpy as np
+import pytest
+import torch
+
+from attn_helpers import DEV, TORCH, check_close, dev, packed_rows
+from fp4_helpers import Fp4Batch, normal, to_dev
+from helpers import elementwise_bound
+from oracle import attn_oracle as A
+from oracle import fp4_oracle as F
+from oracle.ssn_oracle import f64
+from paper_2607_13332_amd import inputs as I
+from paper_2607_13332_amd import ssn
+
+pytestmark = pytest.mark.gpu
+
+# (query heads, key heads, head size, rotated part)
+HEADS = [(40, 8, 128, 128), (16, 16, 64, 64), (3, 1, 256, 256), (4, 2, 128, 64), (6, 3, 32, 32), (3, 2, 96, 24),
+         (5, 1, 160, 0), (2, 2, 1024, 1024), (7, 1, 64, 0)]
+BATCHES = {
+    "one": [(1, 1)],
+    "tokens": [(1, 5), (1, 64), (0, 0), (1, 65), (1, 1000), (0, 9), (1, 128)],
+    "chunks": [(3, 3), (17, 40), (0, 7), (130, 130), (5, 700)],
+    "empty rows": [(2, 1), (1, 0), (5, 2), (1, 3)],
+    "mixed": [(1, 300), (200, 333), (1, 1), (1, 77), (64, 64)],
+}
+
+
+def _rows(bt):
+    """Row numbers and positions of the rows that have one, and their slots."""
+    rows = [(i, b, p) for i, b, p in A.batch_rows(bt.starts, bt.lens) if p >= 0]
+    at, pos = np.array([i for i, _, _ in rows]), np.array([p for _, _, p in rows])
+    return at, pos, (np.array([bt.pages[b, p // bt.page] for _, b, p in rows]), pos % bt.page)
+
+
+def _values(r, shape, dtype):
+    """Normal values, head by head of another size, with rows of special ones."""
+    x = r.standard_normal(shape) * 2.0 ** r.integers(-30, 30, (shape[0], shape[1], 1))
+    x[0, 0] = 0.0
+    x[-1, -1, :32] = np.array([7, -7, 0.25, -0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, -5, 6.96875, 0, -0.0, 1, 2] * 2)
+    x[-1, -1, 0] = 6.96875                        # the group's largest is below 7 in the first half ..
+    x[-1, -1, 1] = -6.96875
+    x[-1, -1, 16:18] = 5.5
+    return I.store(x, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", HEADS)
+def test_values_are_quantised_as_they_are(dtype, heads):
+    """No norm, no rotation: codes and scales bit for bit, nothing else of the
+    caches touched, and read back what they stand for."""
+    Hq, Hk, D, _ = heads
+    for n, (name, page) in enumerate([("one", 16), ("tokens", 16), ("chunks", 64), ("empty rows", 3), ("mixed", 1)]):
+        bt = Fp4Batch(BATCHES[name], Hk, D, page, 5 + n, first=n % 3, pad=n)
+        r = np.random.default_rng(n)
+        k, v = (_values(r, (bt.N, Hk, D), dtype) for _ in range(2))
+        print(f"[case] kv_append_fp4 {dtype} {heads} {name} page={page}", flush=True)
+        args = bt.device()
+        assert ssn.kv_append_fp4(dev(k, dtype), dev(v, dtype), *args, eps=None) is None
+        at, _, slots = _rows(bt)
+        want = [a.copy() for a in bt.held]
+        for z, x in enumerate((k, v)):
+            want[2 * z][slots[0], :, slots[1]], want[2 * z + 1][slots[0], :, slots[1]] = F.quantise(x[at])
+        for name_, got, ref in zip(("Kc", "Ks", "Vc", "Vs"), args, want):
+            assert np.array_equal(got.cpu().numpy(), ref), name_
+        out = [torch.full((bt.N, Hk, D), 7.0, dtype=TORCH[dtype], device=DEV) for _ in range(2)]
+        ssn.kv_read_fp4(*args, bt.N, Kout=out[0], Vout=out[1])
+        rest = np.setdiff1d(np.arange(bt.N), at)
+        for z, got in enumerate(out):
+            got = f64(I.to_host(got))
+            assert np.array_equal(got[at], F.values(want[2 * z], want[2 * z + 1])[slots[0], :, slots[1]])
+            assert (got[rest] == 7).all()
+
+
+def _interval(x, bound, scale):
+    """Codes of x - bound and x + bound under the scales that were written."""
+    e = np.repeat(scale.astype(np.int64) - 127, F.GROUP, -1)
+    lo, hi = np.ldexp(x - bound, -e), np.ldexp(x + bound, -e)
+    size = lambda v: np.sign(v) * F.LEVELS[F.nearest(np.abs(v))]  # noqa: E731
+    return np.ldexp(size(lo), e), np.ldexp(size(hi), e)
+
+
+def _rotated(x, w, pos, table, eps, style):
+    """norm_rope of x, and of its absolute values with all signs positive."""
+    mag = np.abs(A.norm_rope(x, w, eps=eps))
+    if table is not None:
+        R = table.shape[1]
+        c, s = np.abs(table)[pos][:, None, :R // 2], np.abs(table)[pos][:, None, R // 2:]
+        a, b = (slice(0, R // 2), slice(R // 2, R)) if style == "halves" else (slice(0, R, 2), slice(1, R, 2))
+        mag[..., a], mag[..., b] = mag[..., a] * c + mag[..., b] * s, mag[..., a] * s + mag[..., b] * c
+    return A.norm_rope(x, w, pos, table, eps, style), mag
+
+
+@pytest.mark.parametrize("style", ["halves", "pairs"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", HEADS)
+def test_norms_and_rotation_on_the_way(dtype, heads, style):
+    """Keys are quantised from float32: each is what a value within the error
+    bound of the float32 steps becomes, under the scale of a largest one within
+    it.  Queries as kv_append leaves them."""
+    Hq, Hk, D, R = heads
+    table = A.rope_table(1100, R, 5e5).astype(np.float32) if R else None
+    t = None if table is None else to_dev(table)
+    for n, (name, page, eps, weights) in enumerate([("tokens", 16, 1e-6, True), ("mixed", 64, 0.1, True),
+                                                    ("empty rows", 3, 1e-6, False), ("chunks", 7, None, False)]):
+        if eps is None and table is None:
+            continue
+        bt = Fp4Batch(BATCHES[name], Hk, D, page, 5 + n, first=2, pad=3)
+        r = np.random.default_rng(n)
+        q, k, v = (normal(r, (bt.N, h, D), dtype, s) for h, s in ((Hq, 2.0), (Hk, 0.5), (Hk, 1.0)))
+        wq, wk = (I.store(1 + 0.2 * r.standard_normal(D), dtype) if weights else None for _ in range(2))
+        w = [None if a is None else dev(a, dtype) for a in (wq, wk)]
+        print(f"[case] kv_append_fp4 {dtype} {heads} {style} {name} eps={eps}", flush=True)
+        args = bt.device()
+        Qout = torch.full((bt.N, Hq, D), 7.0, dtype=TORCH[dtype], device=DEV)
+        got = ssn.kv_append_fp4(dev(k, dtype), dev(v, dtype), *args, Q=dev(q, dtype), table=t, wq=w[0], wk=w[1], eps=eps,
+                                style=style, Qout=Qout)
+        assert got is Qout
+        at, pos, slots = _rows(bt)
+        ref, mag = _rotated(k[at], wk, pos, table, eps, style)
+        # D / 4 + 8 float32 roundings of the rotated head's absolute values
+        bound = elementwise_bound(ref, mag, D // 4 + 8, False, False)
+        if eps is None:
+            bound[..., R:] = 0.0                  # nothing is computed there
+        codes, scales = (x.cpu().numpy()[slots[0], :, slots[1]] for x in args[:2])
+        low, high = (F.scale_bytes(np.maximum((np.abs(ref) + z * bound).reshape(*ref.shape[:-1], -1, 32).max(-1), 0))
+                     for z in (-1, 1))
+        assert ((low <= scales) & (scales <= high)).all()
+        lo, hi = _interval(ref, bound, scales)
+        x = F.values(codes, scales)
+        assert ((lo <= x) & (x <= hi)).all()
+        # most of them leave no choice
+        assert (lo == hi).mean() > 0.999
+        # nothing else of the caches; values as they are
+        want = [z.copy() for z in bt.held]
+        want[0][slots[0], :, slots[1]], want[1][slots[0], :, slots[1]] = codes, scales
+        want[2][slots[0], :, slots[1]], want[3][slots[0], :, slots[1]] = F.quantise(v[at])
+        for g, z in zip(args, want):
+            assert np.array_equal(g.cpu().numpy(), z)
+        # queries: rounded once
+        ref, mag = _rotated(q[at], wq, pos, table, eps, style)
+        got = I.to_host(Qout)
+        check_close("Qout", got[at], ref, elementwise_bound(ref, mag, D // 4 + 8, False, dtype == "bf16"))
+        assert (f64(got[np.setdiff1d(np.arange(bt.N), at)]) == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [128, 96])
+def test_numbers_at_the_ends_of_the_range(dtype, D):
+    """Groups of denormal numbers, of the largest ones, with infinities and NaN."""
+    r = np.random.default_rng(D)
+    x = r.uniform(-1, 1, (9, 2, D))
+    for i, s in enumerate([2.0 ** -149, 2.0 ** -140, 2.0 ** -133, 2.0 ** -126, 2.0 ** -124, 2.0 ** 127, 3.3e38]):
+        x[i] *= s
+    x = x.astype(np.float32)
+    x[7, 0, 3], x[7, 1, 40], x[8, 0, 31], x[8, 1, 64] = np.inf, -np.inf, np.nan, -np.nan
+    x[8, 0, 0] = np.inf
+    x = I.store(x.astype(np.float64), dtype)
+    bt = Fp4Batch([(9, 12)], 2, D, 5, 3)
+    args = bt.device()
+    ssn.kv_append_fp4(dev(x, dtype), dev(x, dtype), *args, eps=None)
+    codes, scales = F.quantise(x)
+    _, _, slots = _rows(bt)
+    for c, s in (args[:2], args[2:4]):
+        assert np.array_equal(c.cpu().numpy()[slots[0], :, slots[1]], codes)
+        assert np.array_equal(s.cpu().numpy()[slots[0], :, slots[1]], scales)
+    K, V = ssn.kv_read_fp4(*args, 9, dtype=TORCH[dtype])
+    assert np.array_equal(f64(I.to_host(K)), F.values(codes, scales), equal_nan=True) and \
+        torch.equal(torch.nan_to_num(K), torch.nan_to_num(V))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 256, 512])
+def test_every_byte_reads_back(dtype, D):
+    """All codes under all scales."""
+    held = np.arange(256).astype(np.uint8)
+    Hk, page = 2, 16
+    n = 16 * 256
+    codes = np.resize(held, (n, D // 2))
+    scales = np.repeat(held, 16)[:, None].repeat(D // 32, 1)
+    cache = [np.ascontiguousarray(a.reshape(n // page // Hk, Hk, page, -1)) for a in (codes, scales)]
+    npages = n // page // Hk
+    K, V = ssn.kv_read_fp4(*[to_dev(a) for a in cache * 2], to_dev(np.arange(npages, dtype=np.int32)[None]),
+                           to_dev(np.array([0, npages * page], np.int32)), to_dev(np.array([npages * page], np.int32)),
+                           npages * page, dtype=TORCH[dtype])
+    ref = F.values(*cache).transpose(0, 2, 1, 3).reshape(npages * page, Hk, D)
+    if dtype == "bf16":                      # 4 and 6 times 2^126 and 2^127 are past the largest number
+        ref = np.where(np.abs(ref) >= 2.0 ** 128, np.copysign(np.inf, ref), ref)
+    with np.errstate(over="ignore"):
+        ref = ref.astype(np.float32).astype(np.float64)
+    assert np.array_equal(f64(I.to_host(K)), ref, equal_nan=True)
+    assert torch.equal(torch.nan_to_num(K), torch.nan_to_num(V))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("odd", [0, 1])
+@pytest.mark.parametrize("D", [128, 96])
+def test_parts_of_packed_rows(dtype, odd, D):
+    """Strided inputs and outputs; `odd` moves them off the 16-byte grid, and
+    caches to any byte."""
+    bt = Fp4Batch(BATCHES["mixed"], 2, D, 16, 3, pad=1)
+    r = np.random.default_rng(2)
+    k, v = (normal(r, (bt.N, 2, D), dtype) for _ in range(2))
+    args = bt.device()
+    ssn.kv_append_fp4(dev(k, dtype), dev(v, dtype), *args, eps=None)
+    both = packed_rows(np.concatenate([k, v], 1), dtype, ld_extra=64 + odd, before=odd)
+    moved = []
+    for a in bt.held:
+        wide = torch.empty(a.size + 64, dtype=torch.uint8, device=DEV)
+        moved.append(wide[3 * odd:3 * odd + a.size].view(a.shape))
+        moved[-1].copy_(to_dev(a))
+    ssn.kv_append_fp4(both[:, :2], both[:, 2:], *moved, *args[4:], eps=None)
+    for a, b in zip(args, moved):
+        assert torch.equal(a, b)
+    K, V = ssn.kv_read_fp4(*args, bt.N, dtype=TORCH[dtype])
+    out = packed_rows(np.zeros((bt.N, 4, D)).astype(k.dtype), dtype, ld_extra=128 + odd, before=64)
+    ssn.kv_read_fp4(*moved, *args[4:], bt.N, Kout=out[:, :2], Vout=out[:, 2:])
+    last = int(bt.starts[-1])
+    assert torch.equal(out[:last, :2], K[:last]) and torch.equal(out[:last, 2:], V[:last])
+    base = out._base if out._base is not None else out
+    assert (base[:, :64] == 7).all() and (base[:, 64 + 4 * D:] == 7).all() and (out[last:] == 0).all()
+
+
+def test_whole_sequences_move_to_another_cache():
+    """A prefix read back and appended again gives the same bytes."""
+    seqs = [(70, 70), (300, 300), (1, 1)]
+    bt = Fp4Batch(seqs, 2, 64, 16, 3)
+    K, V = ssn.kv_read_fp4(*bt.device(), bt.N)
+    other = Fp4Batch(seqs, 2, 64, 48, 9)
+    args = other.device()
+    ssn.kv_append_fp4(K, V, *args, eps=None)
+    K2, V2 = ssn.kv_read_fp4(*args, bt.N)
+    assert torch.equal(K, K2) and torch.equal(V, V2)
+
+
+def test_rows_past_two_gibi():
+    """Rows 2^31 elements apart, a cache of more than 2^31 codes."""
+    Hk, D, page = 8, 128, 64
+    npages = 2 ** 31 // (Hk * page * D // 2) + 5
+    cache = [torch.zeros((npages, Hk, page, n), dtype=torch.uint8, device=DEV) for n in (D // 2, D // 32) * 2]
+    r = np.random.default_rng(1)
+    k, v = (normal(r, (3, Hk, D), "bf16") for _ in range(2))
+    wide = torch.zeros(2 * 2 ** 31 + 2 * Hk * D, dtype=torch.bfloat16, device=DEV)
+    rows = wide.as_strided((3, 2 * Hk, D), (2 ** 31, D, 1))
+    rows[:, :Hk], rows[:, Hk:] = dev(k, "bf16"), dev(v, "bf16")
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+    batch = (i32([[0, npages - 1]]), i32([0, 3]), i32([page + 2]))
+    ssn.kv_append_fp4(rows[:, :Hk], rows[:, Hk:], *cache, *batch, eps=None)
+    for z, x in enumerate((k, v)):
+        c, s = F.quantise(x)
+        for i, (p, off) in enumerate([(0, page - 1), (npages - 1, 0), (npages - 1, 1)]):
+            assert np.array_equal(cache[2 * z][p, :, off].cpu().numpy(), c[i])
+            assert np.array_equal(cache[2 * z + 1][p, :, off].cpu().numpy(), s[i])
+    rows.zero_()
+    ssn.kv_read_fp4(*cache, *batch, 3, Kout=rows[:, :Hk], Vout=rows[:, Hk:])
+    assert np.array_equal(f64(I.to_host(rows[:, :Hk].contiguous())), F.values(*F.quantise(k)))
+    assert np.array_equal(f64(I.to_host(rows[:, Hk:].contiguous())), F.values(*F.quantise(v)))
+
+
+def test_bounds_below_the_contents_stay_in_bounds():
+    """Row ranges past N, page numbers and lengths out of range: no access
+    outside the buffers (guard bytes around them keep their values)."""
+    bt = Fp4Batch([(5, 300), (40, 90), (1, 1000)], 2, 64, 16, 3)
+    args = bt.device()
+    pages, starts, lens = args[4:]
+    guarded = []
+    for a in bt.held:
+        g = torch.full((a.size + 8192,), 9, dtype=torch.uint8, device=DEV)
+        guarded.append((g, g[4096:4096 + a.size].view(a.shape)))
+    cache = [x for _, x in guarded]
+    K = torch.randn((bt.N, 2, 64), device=DEV).bfloat16()
+    rows = torch.full((bt.N + 64, 4, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = rows[32:32 + bt.N]
+    far = torch.tensor([0, 10 ** 6, -5, 10 ** 9], dtype=torch.int32, device=DEV)
+    for p, s, t in [(pages, far, lens * 1000), (torch.full_like(pages, 10 ** 9), starts, lens),
+                    (torch.full_like(pages, -7), starts, lens - 400)]:
+        ssn.kv_append_fp4(K, K.clone(), *cache, p, s, t)
+        ssn.kv_read_fp4(*cache, p, s, t, bt.N, Kout=out[:, :2], Vout=out[:, 2:])
+    torch.cuda.synchronize()
+    for g, a in guarded:
+        assert (g[:4096] == 9).all() and (g[4096 + a.numel():] == 9).all()
+    assert (rows[:32] == 7).all() and (rows[32 + bt.N:] == 7).all()
+
+
+def test_nothing_to_do():
+    bt = Fp4Batch([(0, 5)], 2, 64, 16, 1)
+    args = bt.device()
+    none = torch.empty((0, 2, 64), dtype=torch.bfloat16, device=DEV)
+    assert ssn.kv_append_fp4(none, none, *args) is None
+    K, V = ssn.kv_read_fp4(*args, 0)
+    assert K.shape == V.shape == (0, 2, 64)
+    for a, b in zip(args, bt.held):
+        assert np.array_equal(a.cpu().numpy(), b)
+
+
+def test_wrappers_refuse():
+    bt = Fp4Batch([(1, 20), (3, 9)], 2, 64, 16, 3)
+    Kc, Ks, Vc, Vs, *batch = bt.device()
+    K = torch.zeros((4, 2, 64), dtype=torch.bfloat16, device=DEV)
+    put = lambda *c, **k: ssn.kv_append_fp4(K, K.clone(), *c, *batch, **k)  # noqa: E731
+    read = lambda *c, **k: ssn.kv_read_fp4(*c, *batch, 4, **k)  # noqa: E731
+    for f in (put, read):
+        with pytest.raises(TypeError, match="Kc must be torch.uint8"):
+            f(Kc.to(torch.int8), Ks, Vc, Vs)
+        with pytest.raises(ValueError, match="shape mismatch"):
+            f(Kc, Ks[..., :1].contiguous(), Vc, Vs)
+        with pytest.raises(ValueError, match="shape mismatch"):
+            f(Kc, Ks, Vc[:-1], Vs)
+        with pytest.raises(ValueError, match="different devices"):
+            f(Kc, Ks.cpu(), Vc, Vs)
+        with pytest.raises(ValueError, match="Vs must be contiguous"):
+            f(Kc, Ks, Vc, Vs.transpose(1, 2).contiguous().transpose(1, 2))
+    with pytest.raises(ssn.SSNError, match="status 7"):          # one cache for both
+        put(Kc, Ks, Kc, Vs)
+    with pytest.raises(ValueError, match="style"):
+        put(Kc, Ks, Vc, Vs, style="thirds")
+    with pytest.raises(TypeError, match="unsupported storage dtype"):
+        read(Kc, Ks, Vc, Vs, dtype=torch.float16)
+    with pytest.raises(TypeError, match="Vout must be"):
+        read(Kc, Ks, Vc, Vs, Kout=K, Vout=K.float())
+    with pytest.raises(ValueError, match="Kout has shape"):
+        read(Kc, Ks, Vc, Vs, Kout=K[:3])
+    with pytest.raises(ValueError, match="multiples of 32"):
+        ssn.fp4_cache(4, 2, 16, 80, DEV)
+    codes, scales = ssn.fp4_cache(4, 2, 16, 96, DEV)
+    assert codes.shape == (4, 2, 16, 48) and scales.shape == (4, 2, 16, 3) and codes.dtype == torch.uint8
