@@ -24,7 +24,8 @@ SOURCES = ["ssn_api.hip", "noalloc.hip", "codec_kernels.hip", "decompress_kernel
            "f32_strips_a.hip", "f32_strips_b.hip", "weights_kernels.hip", "reparam_kernels.hip",
            "sparta_kernels.hip", "attn_api.hip", "rope_kernels.hip", "paged_attn.hip",
            "attn_tiles_bf16.hip", "attn_tiles_f32.hip", "attn_rows_bf16.hip", "attn_rows_f32.hip",
-           "fp4_api.hip", "fp4_cache.hip", "fp4_attn.hip"]
+           "fp4_api.hip", "fp4_cache.hip", "fp4_attn.hip", "fp4_rows_bf16.hip", "fp4_rows_f32.hip",
+           "fp4_tiles_bf16.hip", "fp4_tiles_f32.hip"]
 ARCH = "gfx950"
 
 

@@ -158,7 +158,7 @@ struct RowState {
 // maximum is taken otherwise.  Rows do not touch each other's bits.
 constexpr float kFar = 1024.f;
 __device__ __forceinline__ bool far(float sum, float m) { return !(sum <= kFar) || m == kNegInf; }
-// PARTS of a probability: it as it is rounded, then what the rounding left.
+// PARTS of a probability: it as it is rounded, then what the roundings left.
 template <typename T, int PARTS, int NKB, int QB>
 __device__ __forceinline__ bool probabilities(const f32x4 (&s)[NKB][QB], const float (&m)[QB], float c,
                                               u32x4 (&p)[PARTS][NKB / Mma<T>::kTiles][QB], float (&sum)[QB]) {
@@ -180,7 +180,8 @@ __device__ __forceinline__ bool probabilities(const f32x4 (&s)[NKB][QB], const f
           sum[q] += x[u][i];
         }
       p[0][t][q] = M::probs(x);
-      if constexpr (PARTS == 2) p[1][t][q] = M::remainders(x, p[0][t][q]);
+      if constexpr (PARTS >= 2) p[1][t][q] = M::remainders(x, p[0][t][q]);
+      if constexpr (PARTS == 3) p[2][t][q] = M::last_remainders(x, p[0][t][q], p[1][t][q]);
     }
     any |= far(sum[q], m[q]);
   }
@@ -233,12 +234,14 @@ __device__ __forceinline__ void weigh(const char* vlds, const uint32_t* vb, cons
         odd |= (f[0] ^ v[0]) | (f[1] ^ v[1]) | (f[2] ^ v[2]) | (f[3] ^ v[3]);
         v = f;
       }
-      if constexpr (PARTS == 2) {
+      if constexpr (PARTS >= 2) {
         // (a remainder may be zero or negative: an infinity times it would be NaN
         // or of the other sign)
         const u32x4 f = MASKED ? v : M::bounded(v);
 #pragma unroll
-        for (int q = 0; q < QB; ++q) st.o[d][q] = M::mma(f, p[1][t][q], st.o[d][q]);
+        for (int part = PARTS - 1; part >= 1; --part)
+#pragma unroll
+          for (int q = 0; q < QB; ++q) st.o[d][q] = M::mma(f, p[part][t][q], st.o[d][q]);
       }
 #pragma unroll
       for (int q = 0; q < QB; ++q) st.o[d][q] = M::mma(v, p[0][t][q], st.o[d][q]);

@@ -7,8 +7,8 @@
 // pass over the keys with the running maximum m and sum l of the softmax: for a
 // tile of scores s, m' = max(m, max s), and with a = exp(m - m'), l' = a l + sum
 // exp(s - m'), O' = a O + sum exp(s - m') v; at the end O / l.
+#include "attn_plan.h"
 #include "fp4.h"
-#include "ssn_launch.h"
 
 namespace ssn {
 
@@ -92,16 +92,44 @@ __global__ __launch_bounds__(256) void paged_attn_fp4_generic(Fp4AttnArgs fa) {
   }
 }
 
-size_t fp4_attention_workspace_bytes(int, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t) { return 0; }
+// How a call is run: attn_plan.h.
+size_t fp4_attention_workspace_bytes(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D,
+                                     int64_t max_q, int64_t max_len) {
+  if (D > 256) return 0;
+  const AttnPlan p = attention_plan(dtype, N, B, Hq, Hk, D, max_q, max_len, (size_t)1 << 60);
+  return stage_bytes(p.tiles, D) + stage_bytes(p.rows, D);
+}
 
-hipError_t launch_paged_attention_fp4(int dtype, const Fp4AttnArgs& a, void*, size_t, hipStream_t st) {
-  const int64_t waves = (int64_t)a.a.pb.N * a.a.Hq, blocks = (waves + 3) / 4;
-  const unsigned grid = (unsigned)(blocks > (1 << 20) ? (1 << 20) : blocks);
-  if (dtype == kBF16)
-    hipLaunchKernelGGL((paged_attn_fp4_generic<uint16_t>), dim3(grid), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((paged_attn_fp4_generic<float>), dim3(grid), dim3(256), 0, st, a);
-  return hipGetLastError();
+// The matrix-core kernels read 16 bytes at a time (8 of heads up to 64).
+static bool fp4_vector_access(int dtype, const AttnArgs& a) {
+  const int64_t s = dtype == kBF16 ? 2 : 4;
+  const uintptr_t p = (uintptr_t)a.Q | (uintptr_t)a.Kc | (uintptr_t)a.Vc | (uintptr_t)a.O;
+  return a.D <= 256 && p % 16 == 0 && (a.ldq * s) % 16 == 0 && (a.ldo * s) % 16 == 0;
+}
+
+hipError_t launch_paged_attention_fp4(int dtype, const Fp4AttnArgs& f, void* ws, size_t ws_bytes, hipStream_t st) {
+  const AttnArgs& a = f.a;
+  if (!fp4_vector_access(dtype, a)) {
+    const int64_t waves = (int64_t)a.pb.N * a.Hq, blocks = (waves + 3) / 4;
+    const unsigned grid = (unsigned)(blocks > (1 << 20) ? (1 << 20) : blocks);
+    if (dtype == kBF16)
+      hipLaunchKernelGGL((paged_attn_fp4_generic<uint16_t>), dim3(grid), dim3(256), 0, st, f);
+    else
+      hipLaunchKernelGGL((paged_attn_fp4_generic<float>), dim3(grid), dim3(256), 0, st, f);
+    return hipGetLastError();
+  }
+  AttnPlan p = attention_plan(dtype, a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0);
+  char* at = (char*)ws;
+  for (AttnPart* x : {&p.tiles, &p.rows})
+    if (const size_t bytes = stage_bytes(*x, a.D)) {
+      x->o = (float*)at;
+      x->ml = x->o + x->ranges * x->stage_rows * a.D;
+      at += bytes;
+    }
+  hipError_t e;
+  if (p.tiles.blocks) e = dtype == kBF16 ? launch_fp4_tiles_bf16(f, p, st) : launch_fp4_tiles_f32(f, p, st);
+  else e = dtype == kBF16 ? launch_fp4_rows_bf16(f, p, st) : launch_fp4_rows_f32(f, p, st);
+  return e == hipSuccess ? launch_attn_join(dtype, a, p, st) : e;
 }
 
 }  // namespace ssn

@@ -1,0 +1,88 @@
+// Matrix-core pieces of attention over a 4-bit cache.  Keys and values are exact
+// in bf16, so both products run on the bf16 matrix instructions for either type of
+// Q and O: float32 queries and probabilities go in three bf16 parts, which hold all
+// their bits, against one of K and V.
+#pragma once
+
+#include "attn_mma.h"
+#include "fp4.h"
+
+namespace ssn {
+
+// Storage T of queries and outputs over a 4-bit cache.
+template <typename T>
+struct OverFp4 {};
+template <typename T>
+struct Mma<OverFp4<T>> : Mma<uint16_t> {
+  static constexpr int kQueries = sizeof(T) == 2 ? 1 : 3;     // bf16 parts of a query
+  static constexpr int kRowsParts = sizeof(T) == 2 ? 2 : 3;   // of a probability: rows kernel, tile kernel
+  static constexpr int kTilesParts = sizeof(T) == 2 ? 1 : 3;
+  // what is left after two parts of a probability, exactly
+  __device__ static __forceinline__ u32x4 last_remainders(const f32x4* s, u32x4 p, u32x4 r) {
+    u32x4 l;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      l[i] = pack_bf16x2((s[i >> 1][2 * (i & 1)] - lo_bf16(p[i])) - lo_bf16(r[i]),
+                         (s[i >> 1][2 * (i & 1) + 1] - hi_bf16(p[i])) - hi_bf16(r[i]));
+    return l;
+  }
+  // (the cache has no infinities, and a NaN is one whatever it is multiplied with)
+  __device__ static __forceinline__ u32x4 bounded(u32x4 v) { return v; }
+};
+
+// Eight elements of a query in bf16 parts.  Of float32, the first truncated, so
+// that no finite number becomes infinite; below 2^-110 the last parts run out of
+// bf16's range (an element is then off by 2^-134 at most).
+template <typename T>
+__device__ __forceinline__ void query_parts(const T* p, uint32_t flip, u32x4 (&q)[Mma<OverFp4<T>>::kQueries]) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x4 v = *(const u32x4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[0][i] = v[i] ^ flip;
+  } else {
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const u32x4 v = *(const u32x4*)(p + 4 * z);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t h[2];
+        float r[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t w = v[2 * i + e] ^ flip, a = w & 0x7FFFFFFFu;
+          h[e] = (w & 0xFFFF0000u) | (a > 0x7F800000u ? 0x400000u : 0u);
+          r[e] = a >= 0x7F800000u ? 0.f : __uint_as_float(w) - __uint_as_float(h[e]);
+        }
+        const uint32_t m = pack_bf16x2(r[0], r[1]);
+        q[0][2 * z + i] = (h[0] >> 16) | h[1];
+        q[1][2 * z + i] = m;
+        q[2][2 * z + i] = pack_bf16x2(r[0] - lo_bf16(m), r[1] - hi_bf16(m));
+      }
+    }
+  }
+}
+
+// The NaN that weigh<MASKED> left out of row `scales` of V's scales, for the rows
+// of O that see it.
+template <int DT16, int QB>
+__device__ __forceinline__ void add_nan_groups(const uint8_t* scales, int D, const bool (&sees)[QB],
+                                               RowState<DT16, QB>& st) {
+#pragma unroll
+  for (int d = 0; d < DT16; ++d)
+    if (16 * d < D && scales[d / 2] == kNanScale) {
+#pragma unroll
+      for (int q = 0; q < QB; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[d][q][i] += sees[q] ? __builtin_nanf("") : 0.f;
+    }
+}
+
+// Keys as the lanes of a wave write values to LDS: those of 8 consecutive lanes
+// fall into different columns of 16 bytes (swizzle_values), a chunk each.
+template <int RB>
+__device__ __forceinline__ int value_key(int l) {
+  if constexpr (RB >= 256) return (l & 3) | ((l & 4) << 1) | ((l & 8) >> 1);
+  else return ((l & 7) << 1) | (l >> 3);
+}
+
+}  // namespace ssn

@@ -1,0 +1,207 @@
+// Attention of many rows over a 4-bit cache: a block of 4 waves owns a tile of rows
+// of one sequence and key head (64 QB rows, 16 QB to a wave) and walks the keys the
+// tile sees, 64 (or 32) at a time.  The codes of the tile after the next are on their
+// way to registers, those of the next one become bf16 in LDS, double buffered, while
+// this one's products run.
+#pragma once
+
+#include "attn_tiles.h"
+#include "fp4_attn_mma.h"
+
+namespace ssn {
+
+template <int DT>
+constexpr int fp4_tile_keys() { return DT <= 128 ? 64 : 32; }
+template <int DT>
+constexpr int fp4_tiles_lds() { return 4 * fp4_tile_keys<DT>() * DT * 2; }
+
+template <typename T, int DT, int QB, bool EXACT>
+__device__ __forceinline__ void fp4_tiles_block(const Fp4AttnArgs& fa, const AttnPart& part, int few,
+                                                const TileCount& count, int id, char* mem) {
+  using Tag = OverFp4<T>;
+  using M = Mma<Tag>;
+  constexpr int RB = DT * 2, TK = fp4_tile_keys<DT>(), NC = DT / 32, PARTS = M::kTilesParts, BM = 64 * QB;
+  // keys whose scores are held at a time
+  constexpr int SK = 32, NKB = SK / 16;
+  // A thread fetches a unit of UW dwords of codes, UE elements of one group.
+  constexpr int UPK = 256 / TK, UE = DT / UPK, UW = UE / 8, KPW = kWave / UPK;
+  const AttnArgs& a = fa.a;
+  char(*lds)[2][TK * RB] = (char(*)[2][TK * RB])mem;      // [buffer][K, V]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kh = id % a.Hk, rest = id / a.Hk;
+  if (count.total <= 0) return;
+  const int range = rest / count.total;
+  int b, tile;
+  if (range >= part.ranges ||
+      !count.find(a.pb, a.G, BM, few, balanced_order(rest % count.total, count.total, a.Hk), b, tile))
+    return;
+  const Sequence sq = sequence_of(a.pb, b);
+  const int n = sq.s1 - sq.s0, rows = n * a.G, r0 = tile * BM;
+  const int before = sq.len - n;                           // position of the sequence's token 0
+  const int last = r0 + BM < rows ? r0 + BM - 1 : rows - 1;
+  const int keys = before + last / a.G + 1;                // that the tile sees
+  const int ranges = key_ranges(keys, part.chunk);
+  if (range >= ranges) return;
+
+  const int groups = a.D / kFp4Group;
+  int row[QB], seen[QB];
+  u32x4 qf[QB][NC][M::kQueries];
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    row[q] = r0 + wave * (16 * QB) + q * 16 + (lane & 15);
+    const int r = row[q] < rows ? row[q] : rows - 1, token = r / a.G;
+    seen[q] = before + token;
+    const T* p = (const T*)a.Q + (sq.s0 + token) * a.ldq + (int64_t)(kh * a.G + r % a.G) * a.D;
+#pragma unroll
+    for (int ch = 0; ch < NC; ++ch) {
+      const int e = 32 * ch + 8 * (lane >> 4);
+#pragma unroll
+      for (int m = 0; m < M::kQueries; ++m) qf[q][ch][m] = u32x4{0, 0, 0, 0};
+      if (a.scale != 0.f && (EXACT || e < a.D)) query_parts<T>(p + e, sign_bits<T>(a.scale), qf[q][ch]);
+    }
+  }
+  // a scale of zero: zero queries, any other scale
+  const float c = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * kLog2e;
+  const int wave_last = r0 + (wave + 1) * (16 * QB) - 1;
+  const int seen_hi = before + (wave_last < rows ? wave_last : rows - 1) / a.G;
+
+  const int t0 = range * (part.chunk / TK);
+  const int all = (keys + TK - 1) / TK, t1 = all < t0 + part.chunk / TK ? all : t0 + part.chunk / TK;
+
+  // This thread's key of a tile's keys and of its values, and the unit of both.
+  // Keys past the last repeat it (their scores are masked).
+  const int unit = lane / KPW, e0 = unit * UE;
+  const int k_key = wave * KPW + (lane & (KPW - 1));
+  const int v_key = DT <= 128 ? wave * 16 + value_key<RB>(lane & 15)
+                              : (wave & 1) * 4 + (wave >> 1) * 16 + (lane & 3) + ((lane & 4) << 1);
+  typedef uint32_t piece __attribute__((ext_vector_type(UW)));
+  piece kreg = {}, vreg = {};
+  uint32_t ks = 0, vs = 0;
+  Slot kslot = {0, 0}, vslot = {0, 0};
+  auto find = [&](int t) {
+    const int k = t * TK + k_key, v = t * TK + v_key;
+    kslot = find_slot(a.pb, b, k < keys ? k : keys - 1);
+    vslot = find_slot(a.pb, b, v < keys ? v : keys - 1);
+  };
+  auto fetch = [&]() {
+    const int64_t kr = slot_row(a.pb, kslot, a.Hk, kh), vr = slot_row(a.pb, vslot, a.Hk, kh);
+    if (EXACT || e0 < a.D) {
+      kreg = *(const piece*)((const uint8_t*)a.Kc + kr * (a.D / 2) + e0 / 2);
+      vreg = *(const piece*)((const uint8_t*)a.Vc + vr * (a.D / 2) + e0 / 2);
+      ks = fa.Ks[kr * groups + e0 / kFp4Group];
+      vs = fa.Vs[vr * groups + e0 / kFp4Group];
+    }
+  };
+  auto put_keys = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < UW; ++j)
+      *(u32x4*)(&lds[buf][0][k_key * RB + (((uint32_t)(unit * UW + j) ^ swizzle_keys<RB>(k_key)) << 4)]) =
+          fp4_bf16x8(kreg[j], fp4_scale(ks));
+  };
+  auto put_values = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < UW; ++j)
+      *(u32x4*)(&lds[buf][1][v_key * RB + (((uint32_t)(unit * UW + j) ^ swizzle_values<RB>(v_key)) << 4)]) =
+          fp4_bf16x8(vreg[j], fp4_scale(vs));
+  };
+
+  const uint32_t vb[1] = {M::template vbase<RB>(lane, 0)};
+  const uint32_t kb0 = (lane & 15) * RB + (((uint32_t)(lane >> 4) ^ swizzle_keys<RB>(lane & 15)) << 4);
+
+  RowState<DT / 16, QB> rs;
+  rs.clear();
+  uint32_t odd = 0;
+  // before tile t: its keys and values in LDS, tile t + 1's codes in registers,
+  // tile t + 2's slots
+  if (t0 < t1) {
+    find(t0);
+    fetch();
+    put_keys(0);
+    put_values(0);
+    if (t0 + 1 < t1) {
+      find(t0 + 1);
+      fetch();
+    }
+    if (t0 + 2 < t1) find(t0 + 2);
+  }
+  auto stage = [&](int t) {
+    // the codes of tile t + 1 to LDS, where everyone is done with tile t - 1
+    if (t + 1 < t1) {
+      put_keys((t + 1 - t0) & 1);
+      put_values((t + 1 - t0) & 1);
+    }
+    if (t + 2 < t1) fetch();
+    if (t + 3 < t1) find(t + 3);
+  };
+  constexpr bool kFirst = QB == 3;
+  auto scores = [&](const char* kl, f32x4 (&s)[NKB][QB]) {
+#pragma unroll
+    for (int k = 0; k < NKB; ++k) {
+#pragma unroll
+      for (int q = 0; q < QB; ++q) s[k][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ch = 0; ch < NC; ++ch) {
+        const u32x4 kf = *(const u32x4*)(kl + (kb0 ^ (uint32_t)(ch * 64)) + k * 16 * RB);
+#pragma unroll
+        for (int q = 0; q < QB; ++q)
+#pragma unroll
+          for (int m = M::kQueries - 1; m >= 0; --m) s[k][q] = M::mma(kf, qf[q][ch][m], s[k][q]);
+      }
+    }
+  };
+  // Tiles that every row of the block sees, then the others.
+  const int open = (before + r0 / a.G + 1) / TK, t_open = open < t0 ? t0 : (open < t1 ? open : t1);
+  int t = t0;
+  for (; t < t_open; ++t) {
+    __syncthreads();
+    const char *kl = lds[(t - t0) & 1][0], *vl = lds[(t - t0) & 1][1];
+    stage(t);
+#pragma unroll
+    for (int u = 0; u < TK; u += SK) {
+      f32x4 s[NKB][QB];
+      if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
+      scores(kl + u * RB, s);
+      if constexpr (kFirst) __builtin_amdgcn_s_setprio(0);
+      u32x4 p[PARTS][NKB / 2][QB];
+      softmax_step<Tag, PARTS>(s, rs, c, p);
+      if constexpr (kFirst) __builtin_amdgcn_s_setprio(1);
+      weigh<Tag, RB, false>(vl + u * RB, vb, p, rs, odd);
+      if constexpr (kFirst) __builtin_amdgcn_s_setprio(0);
+    }
+  }
+  for (; t < t1; ++t) {
+    __syncthreads();
+    const char *kl = lds[(t - t0) & 1][0], *vl = lds[(t - t0) & 1][1];
+    stage(t);
+#pragma unroll 1
+    for (int u = 0; u < TK; u += SK) {
+      const int k0 = t * TK + u;
+      if (k0 > seen_hi) break;
+      f32x4 s[NKB][QB];
+      scores(kl + u * RB, s);
+#pragma unroll
+      for (int q = 0; q < QB; ++q)
+#pragma unroll
+        for (int k = 0; k < NKB; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (16 * k + 4 * (lane >> 4) + i > seen[q] - k0) s[k][q][i] = kNegInf;
+      u32x4 p[PARTS][NKB / 2][QB];
+      softmax_step<Tag, PARTS>(s, rs, c, p);
+      weigh<Tag, RB, true>(vl + u * RB, vb, p, rs, odd);
+    }
+  }
+  if (__any(odd != 0)) {
+    // the keys of the masked tiles
+#pragma unroll 1
+    for (int k = t_open * TK; k < t1 * TK && k <= seen_hi; ++k) {
+      bool sees[QB];
+#pragma unroll
+      for (int q = 0; q < QB; ++q) sees[q] = k <= seen[q];
+      add_nan_groups(fa.Vs + (int64_t)cache_row(a.pb, b, a.Hk, kh, k) * groups, a.D, sees, rs);
+    }
+  }
+  finish_rows<T, DT, QB, EXACT>(a, part, rs, row, seen, rows, sq.s0, kh, range, -1, ranges == 1, c, lane);
+}
+
+}  // namespace ssn

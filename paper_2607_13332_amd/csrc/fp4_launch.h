@@ -25,8 +25,13 @@ struct Fp4AttnArgs {
   AttnArgs a;
   const uint8_t *Ks, *Vs;
 };
+// Bytes of workspace that allow every split (0: none).
 size_t fp4_attention_workspace_bytes(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D,
                                      int64_t max_q, int64_t max_len);
+hipError_t launch_fp4_rows_bf16(const Fp4AttnArgs& f, const AttnPlan& p, hipStream_t st);
+hipError_t launch_fp4_rows_f32(const Fp4AttnArgs& f, const AttnPlan& p, hipStream_t st);
+hipError_t launch_fp4_tiles_bf16(const Fp4AttnArgs& f, const AttnPlan& p, hipStream_t st);
+hipError_t launch_fp4_tiles_f32(const Fp4AttnArgs& f, const AttnPlan& p, hipStream_t st);
 hipError_t launch_paged_attention_fp4(int dtype, const Fp4AttnArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
 
 }  // namespace ssn

@@ -47,7 +47,7 @@ class Fp4Batch(Batch):
         return (*[to_dev(a) for a in self.held], to_dev(self.pages), to_dev(self.starts), to_dev(self.lens))
 
 
-def attention_bound(ref, mag, q, kmax, D, scale, length, dtype):
+def attention_bound(ref, mag, q, kmax, vmax, D, scale, length, dtype):
     """Per-element bound of an attention output against the float64 oracle.
 
     Keys and values are exact in the matrix cores' operands.  A score is a
@@ -56,23 +56,26 @@ def attention_bound(ref, mag, q, kmax, D, scale, length, dtype):
     most e = (n + 4) u |scale| |q|_1 kmax (u: unit roundoff of the sums, n: D or
     3 D), and by 2^-22 of itself through the change of base and the exponential,
     and 2^-21 absolute.  A probability is off by twice that (its own and the
-    sum's), by 2^-9 where it is rounded to bf16 (three planes keep a float32 one
-    to 2^-24), and the sums over `length` keys by length u for each part.  All
-    of it multiplies mag = sum p |v|; the output's own rounding is one ulp."""
+    sum's), by 2^-8 where it is rounded to bf16 (8 significant bits, spaced 2^-7 at
+    1, and half of that is the most; three planes keep a float32 one to 2^-24), and the sums over `length` keys by length u for each part.  All
+    of it multiplies mag = sum p |v|.  Exponentials below the smallest normal
+    number, 2^-126, may be flushed to zero: length 2^-126 vmax.  The output's own
+    rounding is one ulp."""
     planes = 1 if dtype == "bf16" else 3
     reach = abs(scale) * np.abs(f64(q)).sum(-1, keepdims=True) * kmax
     e = (planes * D + 4) * U_F32 * reach + 2.0 ** -22 * reach + 2.0 ** -21
-    p = 2.0 * np.expm1(e) + (2.0 ** -9 if dtype == "bf16" else 2.0 ** -23) + 2.0 * planes * length * U_F32
-    return ulp(ref, dtype == "bf16") + p * mag
+    p = 2.0 * np.expm1(e) + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) + 2.0 * planes * length * U_F32
+    return ulp(ref, dtype == "bf16") + p * mag + length * 2.0 ** -126 * vmax
 
 
 def check_attention(bt, Hq, Hk, D, dtype, q, out, lse, scale=None):
     scale = D ** -0.5 if scale is None else scale
     O, L, M = A.paged_attention(q, bt.Kc, bt.Vc, bt.pages, bt.starts, bt.lens, scale)
-    kmax = max([np.abs(A.gather(bt.Kc, bt.pages[b], t)).max(initial=0) for b, t in enumerate(bt.lens)])
+    kmax, vmax = (max([np.abs(A.gather(c, bt.pages[b], t)).max(initial=0) for b, t in enumerate(bt.lens)])
+                  for c in (bt.Kc, bt.Vc))
     inside = ~np.isnan(L[:, 0])
     assert (f64(out[~inside]) == 7).all()
-    bound = attention_bound(O, M, q, kmax, D, scale, bt.max_len, dtype)
+    bound = attention_bound(O, M, q, kmax, vmax, D, scale, bt.max_len, dtype)
     check_close("O", out[inside], O[inside], bound[inside])
     # scores of ordinary size: a flat bar as well
     if inside.any() and scale == D ** -0.5 and np.abs(O[inside]).max(initial=0) > 0:

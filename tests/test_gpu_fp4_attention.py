@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from attn_helpers import DEV, TORCH, check_close, dev, packed_rows
-from fp4_helpers import Fp4Batch, attention_bound, check_attention, normal, to_dev
+from fp4_helpers import Fp4Batch, check_attention, normal, to_dev
 from helpers import U_F32, ulp
 from oracle import attn_oracle as A
 from oracle import fp4_oracle as F
@@ -227,6 +227,38 @@ def test_queries_that_are_not_finite(dtype, new):
     assert np.array_equal(got, want)
 
 
+@pytest.mark.parametrize("new", [1, 33])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lengths_near_the_limit(dtype, new):
+    """2047 x 2^20 keys, every table entry the same page.  Keys are zero, so every
+    probability is one, and values are zeros and ones: the sums over one of 256
+    ranges (8.4 million keys) are whole numbers below 2^24, exact in float32.  Left
+    are 256 additions and multiplications of the join, a division, and of the
+    logarithm (21.5) some units of 2^-20."""
+    page, width, D = 2 ** 20, 2047, 32
+    length = width * page - 5
+    r = np.random.default_rng(3)
+    v = r.integers(0, 2, (page, D)).astype(np.float64)
+    held = [to_dev(a[None, None]) for x in (np.zeros((page, D), np.float32), v.astype(np.float32))
+            for a in F.quantise(x)]
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+    ws = ssn.paged_attention_fp4_workspace(new, 1, 1, 1, D, new, length, DEV, dtype=TORCH[dtype])
+    assert ws is not None
+    q = dev(normal(r, (new, 1, D), dtype), dtype)
+    out = torch.full((new, 1, D), 7e6, dtype=TORCH[dtype], device=DEV)
+    lse = torch.full((new, 1), 7e6, dtype=torch.float32, device=DEV)
+    print(f"[case] attention of {new} tokens over {length} keys", flush=True)
+    ssn.paged_attention_fp4(q, *held, torch.zeros((1, width), dtype=torch.int32, device=DEV), i32([0, new]), i32([length]),
+                            new, length, out=out, lse=lse, workspace=ws)
+    # position t is key t mod 2^20; token i sees length - new + i + 1 of them
+    seen = length - new + 1 + np.arange(new)
+    ones = seen[:, None] // page * v.sum(0) + np.stack([v[:n % page].sum(0) for n in seen])
+    ref = ones / seen[:, None]
+    join = 2 * 256 * U_F32
+    check_close("O", I.to_host(out)[:, 0], ref, ulp(ref, dtype == "bf16") + join * ref)
+    check_close("lse", lse.cpu().numpy()[:, 0], np.log(seen), np.full(new, join + 2.0 ** -17))
+
+
 def test_cache_past_two_gibi():
     """A cache of more than 2^31 codes, its last pages in use."""
     Hk, D, page = 8, 128, 64
@@ -372,7 +404,7 @@ def test_a_quantised_stage_against_a_bf16_one():
     ssn.kv_append(K, V, Kc, Vc, pages, starts, lens, eps=None)
     O4 = ssn.paged_attention_fp4(Q, *cache, pages, starts, lens, bt.max_q, bt.max_len)
     O = ssn.paged_attention(Q, Kc, Vc, pages, starts, lens, bt.max_q, bt.max_len)
-    # both within 2^-9 of the probabilities' sums and a rounding of the exact value
+    # the flat bar of each against the exact value
     assert ((O4.float() - O.float()).norm() / O.float().norm()).item() <= 2 * 3e-3
 
 
