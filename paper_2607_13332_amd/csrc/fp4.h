@@ -52,4 +52,27 @@ __device__ __forceinline__ u32x4 fp4_bf16x8(uint32_t codes, float scale) {
                fp4_bf16x2<3>(codes, scale)};
 }
 
+// The largest of v over LANES (4 or 8) neighbouring lanes, in each of them.
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
+  v = umax(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));     // lane ^ 1
+  v = umax(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));     // lane ^ 2
+  // of 8 lanes the one at the other end: both fours hold theirs everywhere
+  if constexpr (LANES == 8) v = umax(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true));
+  return v;
+}
+// Codes of a lane's E elements (8 or 4) of a group that 32 / E neighbouring lanes
+// hold, and the group's scale byte.
+template <int E>
+__device__ __forceinline__ uint32_t fp4_quantise(const float (&v)[E], uint32_t& s) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) top = umax(top, abs_bits(v[e]));
+  s = fp4_scale_byte(lanes_umax<kFp4Group / E>(top));
+  const float scale = fp4_scale(s);
+  uint32_t codes = fp4_pack<1>(fp4_pack<0>(0, v[0], v[1], scale), v[2], v[3], scale);
+  if constexpr (E == 8) codes = fp4_pack<3>(fp4_pack<2>(codes, v[4], v[5], scale), v[6], v[7], scale);
+  return s == kNanScale ? 0 : codes;
+}
+
 }  // namespace ssn
