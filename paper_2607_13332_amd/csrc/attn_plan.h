@@ -56,8 +56,14 @@ inline int tile_rows(int dtype, int64_t rows, int64_t most, int64_t Hk, int64_t 
   if (D > 64 && (split || rows * Hk / 192 >= 768)) return 3;
   return split || rows * Hk / 128 >= 384 ? 2 : 1;
 }
+// What the rows kernel's ranges aim at: blocks, and the keys of a range a multiple
+// of `unit`.
+struct RowsTuning {
+  int64_t blocks, unit;
+};
+constexpr RowsTuning kRowsTuning = {2048, 128};
 inline AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
-                               int64_t max_len, size_t ws_bytes) {
+                               int64_t max_len, size_t ws_bytes, const RowsTuning& rows_tuning = kRowsTuning) {
   AttnPlan p = {};
   ws_bytes = ws_bytes / 16 * 16;
   const int64_t G = Hq / Hk, most = max_q * G;
@@ -88,8 +94,8 @@ inline AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int6
     // 1 to 4096 keys: 125 / 116 / 105 / 107 / 120 us for 512 / 1024 / 2048 / 4096 /
     // 8192), and no more than 64 ranges to join where 512 blocks have them
     const size_t left = ws_bytes - stage_bytes(p.tiles, D);
-    const int64_t pairs = B * Hk, full = 512 / pairs, want = (2048 + pairs - 1) / pairs;
-    split_keys(p.rows, want > 64 && want > full ? (full > 64 ? full : 64) : want, 128, max_len, D, left);
+    const int64_t pairs = B * Hk, full = 512 / pairs, want = (rows_tuning.blocks + pairs - 1) / pairs;
+    split_keys(p.rows, want > 64 && want > full ? (full > 64 ? full : 64) : want, rows_tuning.unit, max_len, D, left);
   }
   return p;
 }

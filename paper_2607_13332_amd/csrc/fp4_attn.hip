@@ -93,10 +93,15 @@ __global__ __launch_bounds__(256) void paged_attn_fp4_generic(Fp4AttnArgs fa) {
 }
 
 // How a call is run: attn_plan.h.
+// Rows kernel: a block's four waves take 128 keys at a time, and a range of fewer than
+// 256 is mostly the wait for its first.  64 single tokens over caches of 1 to 4096
+// keys take 47 / 43 / 43 / 43 us for 512 / 1024 / 1536 / 2048 blocks, 16 over up to 8192
+// 32 / 26 / 30 / 31: ranges cost their join.
+constexpr RowsTuning kFp4Rows = {1024, 256};
 size_t fp4_attention_workspace_bytes(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D,
                                      int64_t max_q, int64_t max_len) {
   if (D > 256) return 0;
-  const AttnPlan p = attention_plan(dtype, N, B, Hq, Hk, D, max_q, max_len, (size_t)1 << 60);
+  const AttnPlan p = attention_plan(dtype, N, B, Hq, Hk, D, max_q, max_len, (size_t)1 << 60, kFp4Rows);
   return stage_bytes(p.tiles, D) + stage_bytes(p.rows, D);
 }
 
@@ -118,7 +123,7 @@ hipError_t launch_paged_attention_fp4(int dtype, const Fp4AttnArgs& f, void* ws,
       hipLaunchKernelGGL((paged_attn_fp4_generic<float>), dim3(grid), dim3(256), 0, st, f);
     return hipGetLastError();
   }
-  AttnPlan p = attention_plan(dtype, a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0);
+  AttnPlan p = attention_plan(dtype, a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0, kFp4Rows);
   char* at = (char*)ws;
   for (AttnPart* x : {&p.tiles, &p.rows})
     if (const size_t bytes = stage_bytes(*x, a.D)) {

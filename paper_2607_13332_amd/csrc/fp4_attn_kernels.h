@@ -7,16 +7,23 @@
 
 namespace ssn {
 
-// Blocks of a compute unit.
+// Blocks of a compute unit: what its LDS holds, three at most (64 single tokens over
+// caches of 1 to 4096 keys, 8 heads of 128: the rows kernel as it was with queries in
+// registers 49 us with two, 44 with three; with the registers of four it gains
+// nothing).
+constexpr int kUnitLds = 160 * 1024;
 template <typename T, int DT, int QB>
-constexpr int fp4_rows_blocks() { return DT * QB * (int)sizeof(T) <= 512 ? 2 : 1; }
+constexpr int fp4_rows_blocks() {
+  constexpr int n = kUnitLds / fp4_rows_lds<T, DT, QB>();
+  return n < 3 ? n : 3;
+}
 template <typename T, int DT>
 constexpr int fp4_tiles_blocks() { return DT <= 128 ? 2 : 1; }
 
 template <typename T, int DT, int QB, bool EXACT>
 __global__ __launch_bounds__(256, (fp4_rows_blocks<T, DT, QB>())) void paged_attn_fp4_rows(Fp4AttnArgs a,
                                                                                           AttnPart part, int few) {
-  __shared__ __align__(1024) char lds[fp4_rows_lds<DT, QB>()];
+  __shared__ __align__(1024) char lds[fp4_rows_lds<T, DT, QB>()];
   fp4_rows_block<T, DT, QB, EXACT>(a, part, few, blockIdx.x, lds);
 }
 
@@ -35,7 +42,7 @@ constexpr int fp4_both_blocks() { return fp4_rows_blocks<T, DT, 1>() < fp4_tiles
 template <typename T, int DT, int QB, bool EXACT>
 __global__ __launch_bounds__(256, (fp4_both_blocks<T, DT>())) void paged_attn_fp4_both(Fp4AttnArgs a, AttnPlan p,
                                                                                        int slots, int rows) {
-  constexpr int kLds = fp4_tiles_lds<DT>() > fp4_rows_lds<DT, 1>() ? fp4_tiles_lds<DT>() : fp4_rows_lds<DT, 1>();
+  constexpr int kLds = fp4_tiles_lds<DT>() > fp4_rows_lds<T, DT, 1>() ? fp4_tiles_lds<DT>() : fp4_rows_lds<T, DT, 1>();
   __shared__ __align__(1024) char lds[kLds];
   TileCount count;
   count.count(a.a.pb, a.a.G, 64 * QB, p.few, slots);

@@ -30,37 +30,40 @@ struct Mma<OverFp4<T>> : Mma<uint16_t> {
   __device__ static __forceinline__ u32x4 bounded(u32x4 v) { return v; }
 };
 
-// Eight elements of a query in bf16 parts.  Of float32, the first truncated, so
-// that no finite number becomes infinite; below 2^-110 the last parts run out of
-// bf16's range (an element is then off by 2^-134 at most).
+// Eight elements of a query, as they lie in memory (zeros unless `take`), and in
+// bf16 parts.  Of float32 the first part is truncated, so that no finite number
+// becomes infinite; below 2^-110 the last parts run out of bf16's range (an element is
+// then off by 2^-134 at most).
 template <typename T>
-__device__ __forceinline__ void query_parts(const T* p, uint32_t flip, u32x4 (&q)[Mma<OverFp4<T>>::kQueries]) {
-  if constexpr (sizeof(T) == 2) {
-    const u32x4 v = *(const u32x4*)p;
+struct QueryChunk {
+  u32x4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p, bool take) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[0][i] = v[i] ^ flip;
-  } else {
+    for (int z = 0; z < (int)sizeof(T) / 2; ++z) v[z] = take ? *((const u32x4*)p + z) : u32x4{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ void parts(uint32_t flip, u32x4 (&q)[Mma<OverFp4<T>>::kQueries]) const {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const u32x4 v = *(const u32x4*)(p + 4 * z);
+      for (int i = 0; i < 4; ++i) q[0][i] = v[0][i] ^ flip;
+    } else {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 4; ++i) {
         uint32_t h[2];
         float r[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const uint32_t w = v[2 * i + e] ^ flip, a = w & 0x7FFFFFFFu;
+          const uint32_t w = v[i / 2][2 * (i % 2) + e] ^ flip, a = w & 0x7FFFFFFFu;
           h[e] = (w & 0xFFFF0000u) | (a > 0x7F800000u ? 0x400000u : 0u);
           r[e] = a >= 0x7F800000u ? 0.f : __uint_as_float(w) - __uint_as_float(h[e]);
         }
         const uint32_t m = pack_bf16x2(r[0], r[1]);
-        q[0][2 * z + i] = (h[0] >> 16) | h[1];
-        q[1][2 * z + i] = m;
-        q[2][2 * z + i] = pack_bf16x2(r[0] - lo_bf16(m), r[1] - hi_bf16(m));
+        q[0][i] = (h[0] >> 16) | h[1];
+        q[1][i] = m;
+        q[2][i] = pack_bf16x2(r[0] - lo_bf16(m), r[1] - hi_bf16(m));
       }
     }
   }
-}
+};
 
 // The NaN that weigh<MASKED> left out of row `scales` of V's scales, for the rows
 // of O that see it.
@@ -77,12 +80,19 @@ __device__ __forceinline__ void add_nan_groups(const uint8_t* scales, int D, con
     }
 }
 
-// Keys as the lanes of a wave write values to LDS: those of 8 consecutive lanes
-// fall into different columns of 16 bytes (swizzle_values), a chunk each.
+// The row of LDS that holds key l of 16's values: rows of 8 consecutive keys take a
+// chunk each to different columns of 16 bytes (swizzle_values), and those of the 4
+// keys that a transposing read takes a piece of 32 bytes.
 template <int RB>
-__device__ __forceinline__ int value_key(int l) {
+__device__ __forceinline__ int value_row(int l) {
   if constexpr (RB >= 256) return (l & 3) | ((l & 4) << 1) | ((l & 8) >> 1);
   else return ((l & 7) << 1) | (l >> 3);
+}
+// Mma::vbase() with the keys in these rows.
+template <int RB>
+__device__ __forceinline__ uint32_t value_base(int lane) {
+  const int L = lane & 15, row = value_row<RB>(4 * (lane >> 4) + (L >> 2));
+  return row * RB + ((((uint32_t)(L & 3) >> 1) ^ swizzle_values<RB>(row)) << 4) + (L & 1) * 8;
 }
 
 }  // namespace ssn

@@ -55,9 +55,9 @@ __device__ __forceinline__ void fp4_tiles_block(const Fp4AttnArgs& fa, const Att
 #pragma unroll
     for (int ch = 0; ch < NC; ++ch) {
       const int e = 32 * ch + 8 * (lane >> 4);
-#pragma unroll
-      for (int m = 0; m < M::kQueries; ++m) qf[q][ch][m] = u32x4{0, 0, 0, 0};
-      if (a.scale != 0.f && (EXACT || e < a.D)) query_parts<T>(p + e, sign_bits<T>(a.scale), qf[q][ch]);
+      QueryChunk<T> x;
+      x.load(p + e, a.scale != 0.f && (EXACT || e < a.D));
+      x.parts(sign_bits<T>(a.scale), qf[q][ch]);
     }
   }
   // a scale of zero: zero queries, any other scale
@@ -68,44 +68,38 @@ __device__ __forceinline__ void fp4_tiles_block(const Fp4AttnArgs& fa, const Att
   const int t0 = range * (part.chunk / TK);
   const int all = (keys + TK - 1) / TK, t1 = all < t0 + part.chunk / TK ? all : t0 + part.chunk / TK;
 
-  // This thread's key of a tile's keys and of its values, and the unit of both.
-  // Keys past the last repeat it (their scores are masked).
-  const int unit = lane / KPW, e0 = unit * UE;
-  const int k_key = wave * KPW + (lane & (KPW - 1));
-  const int v_key = DT <= 128 ? wave * 16 + value_key<RB>(lane & 15)
-                              : (wave & 1) * 4 + (wave >> 1) * 16 + (lane & 3) + ((lane & 4) << 1);
+  // This thread's key of a tile, and the unit of its codes.  Keys past the last
+  // repeat it (their scores are masked).
+  const int unit = lane / KPW, e0 = unit * UE, key = wave * KPW + (lane & (KPW - 1));
+  const int v_row = (key & ~15) + value_row<RB>(key & 15);
   typedef uint32_t piece __attribute__((ext_vector_type(UW)));
   piece kreg = {}, vreg = {};
   uint32_t ks = 0, vs = 0;
-  Slot kslot = {0, 0}, vslot = {0, 0};
-  auto find = [&](int t) {
-    const int k = t * TK + k_key, v = t * TK + v_key;
-    kslot = find_slot(a.pb, b, k < keys ? k : keys - 1);
-    vslot = find_slot(a.pb, b, v < keys ? v : keys - 1);
-  };
+  Slot slot = {0, 0};
+  auto find = [&](int t) { slot = find_slot(a.pb, b, t * TK + key < keys ? t * TK + key : keys - 1); };
   auto fetch = [&]() {
-    const int64_t kr = slot_row(a.pb, kslot, a.Hk, kh), vr = slot_row(a.pb, vslot, a.Hk, kh);
+    const int64_t row = slot_row(a.pb, slot, a.Hk, kh), c = row * (a.D / 2) + e0 / 2, s = row * groups + e0 / kFp4Group;
     if (EXACT || e0 < a.D) {
-      kreg = *(const piece*)((const uint8_t*)a.Kc + kr * (a.D / 2) + e0 / 2);
-      vreg = *(const piece*)((const uint8_t*)a.Vc + vr * (a.D / 2) + e0 / 2);
-      ks = fa.Ks[kr * groups + e0 / kFp4Group];
-      vs = fa.Vs[vr * groups + e0 / kFp4Group];
+      kreg = *(const piece*)((const uint8_t*)a.Kc + c);
+      vreg = *(const piece*)((const uint8_t*)a.Vc + c);
+      ks = fa.Ks[s];
+      vs = fa.Vs[s];
     }
   };
   auto put_keys = [&](int buf) {
 #pragma unroll
     for (int j = 0; j < UW; ++j)
-      *(u32x4*)(&lds[buf][0][k_key * RB + (((uint32_t)(unit * UW + j) ^ swizzle_keys<RB>(k_key)) << 4)]) =
+      *(u32x4*)(&lds[buf][0][key * RB + (((uint32_t)(unit * UW + j) ^ swizzle_keys<RB>(key)) << 4)]) =
           fp4_bf16x8(kreg[j], fp4_scale(ks));
   };
   auto put_values = [&](int buf) {
 #pragma unroll
     for (int j = 0; j < UW; ++j)
-      *(u32x4*)(&lds[buf][1][v_key * RB + (((uint32_t)(unit * UW + j) ^ swizzle_values<RB>(v_key)) << 4)]) =
+      *(u32x4*)(&lds[buf][1][v_row * RB + (((uint32_t)(unit * UW + j) ^ swizzle_values<RB>(v_row)) << 4)]) =
           fp4_bf16x8(vreg[j], fp4_scale(vs));
   };
 
-  const uint32_t vb[1] = {M::template vbase<RB>(lane, 0)};
+  const uint32_t vb[1] = {value_base<RB>(lane)};
   const uint32_t kb0 = (lane & 15) * RB + (((uint32_t)(lane >> 4) ^ swizzle_keys<RB>(lane & 15)) << 4);
 
   RowState<DT / 16, QB> rs;
