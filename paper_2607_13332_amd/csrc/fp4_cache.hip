@@ -96,30 +96,48 @@ struct KvChunk {
     e = (c - h * per) * 8;
   }
 };
-// Row i's sequence and position; false: it has none.
-__device__ __forceinline__ bool find_row(const PagedBatch& pb, int i, int& b, int& p) {
-  b = sequence_of_row(pb, i);
-  if (b < 0) return false;
-  const Sequence sq = sequence_of(pb, b);
-  p = sq.len - (sq.s1 - i);
-  return i < sq.s1 && p >= 0;
-}
+// The batch's sequences as a wave looks rows up in them.  Of up to 64 a lane has one,
+// all loaded at once, and a lookup waits for nothing; of more every lookup searches
+// memory.
+struct Sequences {
+  int s0, s1, len;      // of sequence `lane`
+  __device__ __forceinline__ void load(const PagedBatch& pb) {
+    const int lane = threadIdx.x & 63, b = lane < pb.B ? lane : pb.B - 1;
+    if (pb.B > kWave) return;
+    s0 = pb.starts[b];
+    s1 = pb.starts[b + 1];
+    len = pb.lens[b];
+  }
+  // The sequence of row i, its number b; -1 before the first.
+  __device__ __forceinline__ Sequence find(const PagedBatch& pb, int i, int& b) const {
+    if (pb.B > kWave) {
+      b = sequence_of_row(pb, i);
+      return b < 0 ? Sequence{0, 0, 0} : sequence_of(pb, b);
+    }
+    const int lane = threadIdx.x & 63;
+    b = __popcll(__ballot(lane < pb.B && s0 <= i)) - 1;
+    Sequence sq = {0, 0, 0};
+    if (b >= 0) {
+      sq.s0 = clampi(__builtin_amdgcn_readlane(s0, b), 0, pb.N);
+      sq.s1 = clampi(__builtin_amdgcn_readlane(s1, b), sq.s0, pb.N);
+      sq.len = clampi(__builtin_amdgcn_readlane(len, b), 0, pb.max_len);
+    }
+    return sq;
+  }
+};
 
 // The cache rows of head h at the positions of U consecutive rows from i on; -1:
 // a row has none.  Rows of one sequence follow from the first.
 template <int U>
-__device__ __forceinline__ void find_rows(const PagedBatch& pb, int i, int Hk, int h, int64_t (&row)[U]) {
-  int b = sequence_of_row(pb, i);
-  Sequence sq = {0, 0, 0};
-  if (b >= 0) sq = sequence_of(pb, b);
+__device__ __forceinline__ void find_rows(const PagedBatch& pb, const Sequences& seqs, int i, int Hk, int h,
+                                          int64_t (&row)[U]) {
+  int b;
+  Sequence sq = seqs.find(pb, i, b);
   bool has[U];
   Slot slot[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (u && i + u < pb.N && (b < 0 || i + u >= sq.s1)) {
-      b = sequence_of_row(pb, i + u);
-      if (b >= 0) sq = sequence_of(pb, b);
-    }
+    if (u && i + u < pb.N && (b < 0 || i + u >= sq.s1)) sq = seqs.find(pb, i + u, b);
     const int p = sq.len - (sq.s1 - (i + u));
     has[u] = b >= 0 && i + u < sq.s1 && p >= 0;
     slot[u] = Slot{0, 0};
@@ -142,6 +160,8 @@ __global__ __launch_bounds__(256) void kv_append_fp4_plain(Spread sp, PagedBatch
   const HeadRows in = at.isv ? v : k;
   const T* src = (const T*)in.p + at.h * D + at.e;
   uint8_t *codes = at.isv ? c.Vc : c.Kc, *scales = at.isv ? c.Vs : c.Ks;
+  Sequences seqs;
+  seqs.load(pb);
   for (int64_t i = (int64_t)(id / sp.passes) * U; i < pb.N; i += (int64_t)sp.slots * U) {
     Chunk<uint16_t> x[U];               // 8 elements of either type
 #pragma unroll
@@ -157,7 +177,7 @@ __global__ __launch_bounds__(256) void kv_append_fp4_plain(Spread sp, PagedBatch
       }
     }
     int64_t row[U];
-    find_rows<U>(pb, (int)i, k.H, at.h, row);
+    find_rows<U>(pb, seqs, (int)i, k.H, at.h, row);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       uint32_t s;
@@ -195,9 +215,13 @@ __global__ __launch_bounds__(256) void kv_append_fp4_rows(Spread sp, NormRope nr
     wa.set(*(const u32x4*)(w + E * j));
     wb.set(*(const u32x4*)(w + D / 2 + E * j));
   }
+  Sequences seqs;
+  seqs.load(pb);
   for (int i = id / sp.passes; i < pb.N; i += sp.slots) {
-    int b, p;
-    if (!find_row(pb, i, b, p)) continue;
+    int b;
+    const Sequence sq = seqs.find(pb, i, b);
+    const int p = sq.len - (sq.s1 - i);
+    if (b < 0 || i >= sq.s1 || p < 0) continue;
     u32x4 xa = {0, 0, 0, 0}, xb = {0, 0, 0, 0};
     if (any) {
       xa = __builtin_nontemporal_load((const u32x4*)(src + i * in.ld));
@@ -258,9 +282,11 @@ __global__ __launch_bounds__(256) void kv_read_fp4_rows(Spread sp, PagedBatch pb
   const HeadRows out = at.isv ? v : k;
   T* dst = (T*)out.p + at.h * D + at.e;
   const uint8_t *codes = at.isv ? c.Vc : c.Kc, *scales = at.isv ? c.Vs : c.Ks;
+  Sequences seqs;
+  seqs.load(pb);
   for (int64_t i = (int64_t)(id / sp.passes) * U; i < pb.N; i += (int64_t)sp.slots * U) {
     int64_t row[U];
-    find_rows<U>(pb, (int)i, k.H, at.h, row);
+    find_rows<U>(pb, seqs, (int)i, k.H, at.h, row);
     uint32_t w[U], e[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -288,9 +314,12 @@ __global__ __launch_bounds__(256) void kv_read_fp4_rows(Spread sp, PagedBatch pb
 }
 
 static bool codes_aligned(const Fp4Cache& c) { return ((uintptr_t)c.Kc | (uintptr_t)c.Vc) % 4 == 0; }
-// Tokens that a wave has at a time: four where there are waves enough.
-constexpr int kTokens = 4;
-static bool tokens_by_four(const PagedBatch& pb, int Hk, int D) { return (int64_t)pb.N * Hk * D >= kForwardWaves * 256; }
+// Tokens that a wave has at a time, one where there would be too few waves.  29.5k
+// tokens of 8 heads of 128 are read back in 42 / 38 / 36 us with 2 / 4 / 8, 131072 in
+// 178 / 159 / 138 (4.9 TB/s, the rate of a large copy); appends gain 1 % from more
+// than 4.  (69 us with one and a search in memory for each, 41 with four of those.)
+constexpr int kAppendTokens = 4, kReadTokens = 8;
+static bool many_tokens(const PagedBatch& pb, int Hk, int D) { return (int64_t)pb.N * Hk * D >= kForwardWaves * 256; }
 static Spread spread_chunks(int64_t tokens, int Hk, int D) {
   return spread_tokens(tokens, 2 * Hk * (D / 8), kWave, kForwardWaves);
 }
@@ -322,9 +351,9 @@ static hipError_t append(const Fp4Append& a) {
   constexpr int kType = sizeof(T) == 2 ? kBF16 : kF32;
   const bool codes = codes_aligned(a.c);
   if (codes && a.q.H == 0 && a.nr.eps < 0.f && a.nr.R == 0 && aligned16(a.k, sizeof(T)) && aligned16(a.v, sizeof(T))) {
-    if (tokens_by_four(a.pb, a.k.H, a.nr.D)) {
-      const Spread sp = spread_chunks((a.pb.N + kTokens - 1) / kTokens, a.k.H, a.nr.D);
-      hipLaunchKernelGGL((kv_append_fp4_plain<T, kTokens>), grid_of(sp), dim3(256), 0, a.st, sp, a.pb, a.nr.D, a.k, a.v, a.c);
+    if (many_tokens(a.pb, a.k.H, a.nr.D)) {
+      const Spread sp = spread_chunks((a.pb.N + kAppendTokens - 1) / kAppendTokens, a.k.H, a.nr.D);
+      hipLaunchKernelGGL((kv_append_fp4_plain<T, kAppendTokens>), grid_of(sp), dim3(256), 0, a.st, sp, a.pb, a.nr.D, a.k, a.v, a.c);
     } else {
       const Spread sp = spread_chunks(a.pb.N, a.k.H, a.nr.D);
       hipLaunchKernelGGL((kv_append_fp4_plain<T, 1>), grid_of(sp), dim3(256), 0, a.st, sp, a.pb, a.nr.D, a.k, a.v, a.c);
@@ -350,9 +379,9 @@ hipError_t launch_kv_append_fp4(int dtype, const PagedBatch& pb, const NormRope&
 template <typename T>
 static hipError_t read_back(const PagedBatch& pb, int D, const Fp4Cache& c, HeadRows k, HeadRows v, hipStream_t st) {
   if (codes_aligned(c) && aligned16(k, sizeof(T)) && aligned16(v, sizeof(T))) {
-    if (tokens_by_four(pb, k.H, D)) {
-      const Spread sp = spread_chunks((pb.N + kTokens - 1) / kTokens, k.H, D);
-      hipLaunchKernelGGL((kv_read_fp4_rows<T, kTokens>), grid_of(sp), dim3(256), 0, st, sp, pb, D, c, k, v);
+    if (many_tokens(pb, k.H, D)) {
+      const Spread sp = spread_chunks((pb.N + kReadTokens - 1) / kReadTokens, k.H, D);
+      hipLaunchKernelGGL((kv_read_fp4_rows<T, kReadTokens>), grid_of(sp), dim3(256), 0, st, sp, pb, D, c, k, v);
     } else {
       const Spread sp = spread_chunks(pb.N, k.H, D);
       hipLaunchKernelGGL((kv_read_fp4_rows<T, 1>), grid_of(sp), dim3(256), 0, st, sp, pb, D, c, k, v);
