@@ -56,12 +56,13 @@ inline int tile_rows(int dtype, int64_t rows, int64_t most, int64_t Hk, int64_t 
   if (D > 64 && (split || rows * Hk / 192 >= 768)) return 3;
   return split || rows * Hk / 128 >= 384 ? 2 : 1;
 }
-// What the rows kernel's ranges aim at: blocks, and the keys of a range a multiple
-// of `unit`.
+// What ranges aim at: `blocks` of the rows kernel, the keys of a range a multiple of
+// `unit` and no fewer than `least` for each pair of a sequence and a key head (2048
+// suffice), and `beside` blocks of the tile kernel where a launch has both.
 struct RowsTuning {
-  int64_t blocks, unit;
+  int64_t blocks, unit, least, beside;
 };
-constexpr RowsTuning kRowsTuning = {2048, 128};
+constexpr RowsTuning kRowsTuning = {2048, 128, 0, 512};
 inline AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
                                int64_t max_len, size_t ws_bytes, const RowsTuning& rows_tuning = kRowsTuning) {
   AttnPlan p = {};
@@ -82,7 +83,8 @@ inline AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int6
     // tokens over 32768 keys: 497 us for 256 blocks, 317 for 512, 315 for 1024;
     // four chunks of up to 100 over 8192: 105, 76, 87)
     const int64_t blocks = (rows / (64 * p.tiles.blocks) + 1) * Hk;
-    int64_t want = blocks >= 512 ? 1 : 512 / blocks;
+    const int64_t full = p.rows.blocks ? rows_tuning.beside : 512;
+    int64_t want = blocks >= full ? 1 : full / blocks;
     // as many as the grid holds: it has a block for every range of every number a
     // tile may have, and sequences without new tokens have numbers too
     const int64_t most_ranges = kMaxTileBlocks / (tile_slots(N, B, G, 64 * p.tiles.blocks) * Hk);
@@ -95,7 +97,10 @@ inline AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int6
     // 8192), and no more than 64 ranges to join where 512 blocks have them
     const size_t left = ws_bytes - stage_bytes(p.tiles, D);
     const int64_t pairs = B * Hk, full = 512 / pairs, want = (rows_tuning.blocks + pairs - 1) / pairs;
-    split_keys(p.rows, want > 64 && want > full ? (full > 64 ? full : 64) : want, rows_tuning.unit, max_len, D, left);
+    int64_t ranges = want > 64 && want > full ? (full > 64 ? full : 64) : want;
+    const int64_t least = rows_tuning.least * pairs < 2048 ? rows_tuning.least * pairs : 2048;
+    if (least && ranges > max_len / least) ranges = max_len / least > 1 ? max_len / least : 1;
+    split_keys(p.rows, ranges, rows_tuning.unit, max_len, D, left);
   }
   return p;
 }

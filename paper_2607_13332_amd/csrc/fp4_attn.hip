@@ -95,9 +95,17 @@ __global__ __launch_bounds__(256) void paged_attn_fp4_generic(Fp4AttnArgs fa) {
 // How a call is run: attn_plan.h.
 // Rows kernel: a block's four waves take 128 keys at a time, and a range of fewer than
 // 256 is mostly the wait for its first.  64 single tokens over caches of 1 to 4096
-// keys take 47 / 43 / 43 / 43 us for 512 / 1024 / 1536 / 2048 blocks, 16 over up to 8192
-// 32 / 26 / 30 / 31: ranges cost their join.
-constexpr RowsTuning kFp4Rows = {1024, 256};
+// keys (8 heads of 128) take 47 / 43 / 43 / 43 us for 512 / 1024 / 1536 / 2048 blocks,
+// 16 over up to 8192 32 / 26 / 30 / 31.  Ranges cost their join, 4 us and more, which
+// shorter ones do not give back where the pairs fill the chip by themselves: 64
+// sequences of up to 512 / 1024 / 2048 / 4096 keys take 12 / 16 / 27 / 48 us with one
+// range each and 20 / 24 / 33 / 44 with ranges for 1024 blocks.
+//
+// Beside the rows' blocks tiles do not need the whole chip: 517 tokens and 31 single
+// ones over up to 8192 keys take 150 / 121 / 125 us with 256 / 384 / 512 blocks, 256
+// tokens and 63 over up to 4096 87 / 90 / 97, 200 tokens and 15 over up to 32768 195 /
+// 195 / 207.
+constexpr RowsTuning kFp4Rows = {1024, 256, 4, 384};
 size_t fp4_attention_workspace_bytes(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D,
                                      int64_t max_q, int64_t max_len) {
   if (D > 256) return 0;
