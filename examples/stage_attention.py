@@ -1,12 +1,14 @@
 """One pipeline stage's attention sublayer, as it answers and as it trains.
 
-    python examples/stage_attention.py [--tokens 16]
+    python examples/stage_attention.py [--tokens 16] [--fp4]
 
 Serving: coordinates arrive, are decompressed, give queries, keys and values;
 ``kv_append`` norms and rotates them and files keys and values in a paged cache,
 ``paged_attention`` reads it, the reparameterized output projection adds to the
 residual stream, and the coordinates of the result leave.  Prompts go through in
-chunks, then every sequence advances a token at a time.
+chunks, then every sequence advances a token at a time.  With --fp4 the cache holds
+4 bits an element (``kv_append_fp4``, ``paged_attention_fp4``); ``move`` takes a
+sequence of it to another cache (``kv_read_fp4``).
 
 Training: ``qk_norm_rope`` and its backward as a torch autograd function.
 """
@@ -48,9 +50,12 @@ class Stage:
         X = ssn.decompress(Z, ids, self.E, self.U)
         q, k, v = self.heads(X)
         pages, starts, lens, max_q, max_len = batch
-        q = ssn.kv_append(k, v, *cache, pages, starts, lens, Q=q, table=self.table, wq=self.wq, wk=self.wk)
-        ws = ssn.paged_attention_workspace(X.shape[0], pages.shape[0], self.Hq, self.Hk, self.D, max_q, max_len, DEV)
-        O = ssn.paged_attention(q, *cache, pages, starts, lens, max_q, max_len, workspace=ws)
+        append, attention, workspace = ssn.kv_append, ssn.paged_attention, ssn.paged_attention_workspace
+        if len(cache) == 4:            # codes and scales of keys and of values
+            append, attention, workspace = ssn.kv_append_fp4, ssn.paged_attention_fp4, ssn.paged_attention_fp4_workspace
+        q = append(k, v, *cache, pages, starts, lens, Q=q, table=self.table, wq=self.wq, wk=self.wk)
+        ws = workspace(X.shape[0], pages.shape[0], self.Hq, self.Hk, self.D, max_q, max_len, DEV)
+        O = attention(q, *cache, pages, starts, lens, max_q, max_len, workspace=ws)
         _, Y = ssn.reparam_forward(O.view(X.shape[0], -1), self.Zp, self.U)
         return ssn.compress(X + Y, ids, self.E, self.U)
 
@@ -58,9 +63,12 @@ class Stage:
 class Pages:
     """Pages of one layer's cache, handed out as sequences grow."""
 
-    def __init__(self, stage, npages, size, B):
+    def __init__(self, stage, npages, size, B, fp4=False):
         shape = (npages, stage.Hk, size, stage.D)
-        self.cache = [torch.empty(shape, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        if fp4:
+            self.cache = [*ssn.fp4_cache(*shape, DEV), *ssn.fp4_cache(*shape, DEV)]
+        else:
+            self.cache = [torch.empty(shape, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
         self.size, self.free = size, list(range(npages))
         self.lens = [0] * B
         self.table = [[] for _ in range(B)]
@@ -93,14 +101,29 @@ class QKNormRope(torch.autograd.Function):
         return gq, gk, gwq.to(wq.dtype), gwk.to(wk.dtype), None, None
 
 
-def serve(tokens=16, prompts=(300, 41, 700), chunk=256):
+def move(cache, pages, length, size):
+    """A sequence of a 4-bit cache, its page numbers [1, width], into a cache of
+    its own with pages of another size: read back, appended as it is.  Returns
+    that cache and its page numbers."""
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    rows = (i32([0, length]), i32([length]))
+    K, V = ssn.kv_read_fp4(*cache, pages, *rows, length)
+    need = -(-length // size)
+    shape = (need, K.shape[1], size, K.shape[2])
+    other = [*ssn.fp4_cache(*shape, DEV), *ssn.fp4_cache(*shape, DEV)]
+    numbers = i32([list(range(need))])
+    ssn.kv_append_fp4(K, V, *other, numbers, *rows, eps=None)
+    return other, numbers
+
+
+def serve(tokens=16, prompts=(300, 41, 700), chunk=256, fp4=False):
     """Coordinates of each sequence's last token: fed in chunks and then token
     by token, and fed whole."""
     stage = Stage()
     g = torch.Generator(device=DEV).manual_seed(1)
     ids = [torch.randint(0, 1000, (n + tokens,), generator=g, device=DEV, dtype=torch.int32) for n in prompts]
     Z = [torch.randn((len(i), 64), generator=g, device=DEV) for i in ids]
-    pages = Pages(stage, 200, 16, len(prompts))
+    pages = Pages(stage, 200, 16, len(prompts), fp4)
     done = [0] * len(prompts)
     total = [len(i) for i in ids]
     out = [None] * len(prompts)
@@ -114,7 +137,7 @@ def serve(tokens=16, prompts=(300, 41, 700), chunk=256):
             if new[b]:
                 out[b] = part[-1]
         done = [d + n for d, n in zip(done, new)]
-    whole = Pages(stage, 200, 16, len(prompts))
+    whole = Pages(stage, 200, 16, len(prompts), fp4)
     z = stage.serve(torch.cat(Z), torch.cat(ids), whole.cache, whole.batch(total))
     return torch.stack(out), torch.stack([part[-1] for part in z.split(total)])
 
@@ -138,10 +161,14 @@ def train():
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--tokens", type=int, default=16)
+    ap.add_argument("--fp4", action="store_true", help="a cache of 4 bits an element")
     a = ap.parse_args()
-    steps, whole = serve(a.tokens)
+    steps, whole = serve(a.tokens, fp4=a.fp4)
     print(f"serving: chunks and {a.tokens} single tokens against whole prompts: "
           f"rel {((steps - whole).norm() / whole.norm()).item():.2e}")
+    if a.fp4:
+        stored = serve(a.tokens)[1]
+        print(f"serving: the 4-bit cache against the bf16 one: rel {((whole - stored).norm() / stored.norm()).item():.2e}")
     loss, norms = train()
     print(f"training: loss {loss:.4f}, gradient norms " + ", ".join(f"{n:.3e}" for n in norms))
 

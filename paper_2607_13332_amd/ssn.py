@@ -896,10 +896,10 @@ def fp4_cache(npages: int, Hk: int, page_size: int, D: int, device) -> tuple:
 
 def _paged_fp4(Kc, Ks, Vc, Vs, pages, starts, lens, first, g, Hk, D):
     """(B, C arguments) of a batch of sequences over the 4-bit cache."""
-    kc = Kc.shape
+    kc, ks = Kc.shape, Ks.shape
     if len(kc) != 4 or D % FP4_GROUP or kc[1] != Hk or kc[3] != D // 2 or Vc.shape != kc or \
-            Ks.shape != (*kc[:3], D // FP4_GROUP) or Vs.shape != Ks.shape:
-        raise ValueError(f"shape mismatch Kc{tuple(kc)} Ks{tuple(Ks.shape)} Vc{tuple(Vc.shape)} Vs{tuple(Vs.shape)}, "
+            ks != (kc[0], Hk, kc[2], D // FP4_GROUP) or Vs.shape != ks:
+        raise ValueError(f"shape mismatch Kc{tuple(kc)} Ks{tuple(ks)} Vc{tuple(Vc.shape)} Vs{tuple(Vs.shape)}, "
                          f"expected codes (pages, {Hk}, page_size, {D} / 2) and scales "
                          f"(pages, {Hk}, page_size, {D} / {FP4_GROUP})")
     if pages.dim() != 2:
@@ -909,9 +909,17 @@ def _paged_fp4(Kc, Ks, Vc, Vs, pages, starts, lens, first, g, Hk, D):
         raise ValueError(f"shape mismatch pages{tuple(pages.shape)} starts{tuple(starts.shape)} "
                          f"lens{tuple(lens.shape)}")
     u8, i32 = torch.uint8, torch.int32
-    return B, (_gpu(Kc, "Kc", first, g, u8, 4), _gpu(Ks, "Ks", first, g, u8, 4), _gpu(Vc, "Vc", first, g, u8, 4),
-               _gpu(Vs, "Vs", first, g, u8, 4), kc[0], kc[2], _gpu(pages, "pages", first, g, i32, 2), width,
-               _gpu(starts, "starts", first, g, i32, 1), _gpu(lens, "lens", first, g, i32, 1))
+    # what _gpu looks at, in one go (seven calls take a microsecond more)
+    ok = g >= 0 and starts.dim() == lens.dim() == 1
+    for t, dt in ((Kc, u8), (Ks, u8), (Vc, u8), (Vs, u8), (pages, i32), (starts, i32), (lens, i32)):
+        ok = ok and t.get_device() == g and t.dtype is dt and t.is_contiguous()
+    if not ok:
+        for t, name in ((Kc, "Kc"), (Ks, "Ks"), (Vc, "Vc"), (Vs, "Vs")):
+            _gpu(t, name, first, g, u8, 4)
+        for t, name, n in ((pages, "pages", 2), (starts, "starts", 1), (lens, "lens", 1)):
+            _gpu(t, name, first, g, i32, n)
+    return B, (Kc.data_ptr(), Ks.data_ptr(), Vc.data_ptr(), Vs.data_ptr(), kc[0], kc[2], pages.data_ptr(), width,
+               starts.data_ptr(), lens.data_ptr())
 
 
 def kv_append_fp4(K: torch.Tensor, V: torch.Tensor, Kc: torch.Tensor, Ks: torch.Tensor, Vc: torch.Tensor,

@@ -224,6 +224,33 @@ def test_parts_of_packed_rows(dtype, odd, D):
     assert (base[:, :64] == 7).all() and (base[:, 64 + 4 * D:] == 7).all() and (out[last:] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [63, 64, 65, 300])
+def test_many_sequences(dtype, B):
+    """Ragged batches on both sides of the sequences that a wave holds, empty ones
+    at the ends and between, tokens enough for more than one to a wave."""
+    r = np.random.default_rng(B)
+    seqs = [(0, 3)] + [(int(n), int(n) + int(r.integers(0, 9))) for n in r.choice([0, 1, 2, 5, 300], B - 2)] + [(0, 0)]
+    bt = Fp4Batch(seqs, 8, 128, 16, 3, first=3, pad=2)
+    assert bt.N * 8 * 128 >= 2 ** 23 or B < 100
+    k, v = (normal(r, (bt.N, 8, 128), dtype) for _ in range(2))
+    args = bt.device()
+    ssn.kv_append_fp4(dev(k, dtype), dev(v, dtype), *args, eps=None)
+    at, _, slots = _rows(bt)
+    want = [a.copy() for a in bt.held]
+    for z, x in enumerate((k, v)):
+        want[2 * z][slots[0], :, slots[1]], want[2 * z + 1][slots[0], :, slots[1]] = F.quantise(x[at])
+    for got, ref in zip(args, want):
+        assert np.array_equal(got.cpu().numpy(), ref)
+    out = [torch.full((bt.N, 8, 128), 7.0, dtype=TORCH[dtype], device=DEV) for _ in range(2)]
+    ssn.kv_read_fp4(*args, bt.N, Kout=out[0], Vout=out[1])
+    rest = np.setdiff1d(np.arange(bt.N), at)
+    for z, got in enumerate(out):
+        got = f64(I.to_host(got))
+        assert np.array_equal(got[at], F.values(want[2 * z], want[2 * z + 1])[slots[0], :, slots[1]])
+        assert (got[rest] == 7).all()
+
+
 def test_whole_sequences_move_to_another_cache():
     """A prefix read back and appended again gives the same bytes."""
     seqs = [(70, 70), (300, 300), (1, 1)]
