@@ -56,15 +56,20 @@ inline int tile_rows(int dtype, int64_t rows, int64_t most, int64_t Hk, int64_t 
   if (D > 64 && (split || rows * Hk / 192 >= 768)) return 3;
   return split || rows * Hk / 128 >= 384 ? 2 : 1;
 }
-// What ranges aim at: `blocks` of the rows kernel, the keys of a range a multiple of
-// `unit` and no fewer than `least` for each pair of a sequence and a key head (2048
-// suffice), and `beside` blocks of the tile kernel where a launch has both.
-struct RowsTuning {
+// How a kernel's calls are cut: `blocks` of the rows kernel that ranges aim at, the keys
+// of a range a multiple of `unit` and no fewer than `least` for each pair of a sequence
+// and a key head (2048 suffice); `beside` blocks of the tile kernel where a launch has
+// both; and its 16-row blocks of a wave.
+struct AttnTuning {
   int64_t blocks, unit, least, beside;
+  int (*tile_rows)(int dtype, int64_t rows, int64_t most, int64_t max_q, int64_t Hk, int64_t D, int64_t max_len);
 };
-constexpr RowsTuning kRowsTuning = {2048, 128, 0, 512};
+inline int stored_tile_rows(int dtype, int64_t rows, int64_t most, int64_t, int64_t Hk, int64_t D, int64_t max_len) {
+  return tile_rows(dtype, rows, most, Hk, D, max_len);
+}
+constexpr AttnTuning kStoredTuning = {2048, 128, 0, 512, stored_tile_rows};
 inline AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_q,
-                               int64_t max_len, size_t ws_bytes, const RowsTuning& rows_tuning = kRowsTuning) {
+                               int64_t max_len, size_t ws_bytes, const AttnTuning& tuning = kStoredTuning) {
   AttnPlan p = {};
   ws_bytes = ws_bytes / 16 * 16;
   const int64_t G = Hq / Hk, most = max_q * G;
@@ -78,12 +83,12 @@ inline AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int6
   p.tiles.stage_rows = N * Hq;
   if (tiles) {
     const int64_t rows = (p.few && N - B >= 0 ? N - B + 1 : N) * G;
-    p.tiles.blocks = tile_rows(dtype, rows, most, Hk, D, max_len);
+    p.tiles.blocks = tuning.tile_rows(dtype, rows, most, max_q, Hk, D, max_len);
     // two blocks to a compute unit, where the rows alone do not give them (512
     // tokens over 32768 keys: 497 us for 256 blocks, 317 for 512, 315 for 1024;
     // four chunks of up to 100 over 8192: 105, 76, 87)
     const int64_t blocks = (rows / (64 * p.tiles.blocks) + 1) * Hk;
-    const int64_t full = p.rows.blocks ? rows_tuning.beside : 512;
+    const int64_t full = p.rows.blocks ? tuning.beside : 512;
     int64_t want = blocks >= full ? 1 : full / blocks;
     // as many as the grid holds: it has a block for every range of every number a
     // tile may have, and sequences without new tokens have numbers too
@@ -96,11 +101,11 @@ inline AttnPlan attention_plan(int dtype, int64_t N, int64_t B, int64_t Hq, int6
     // 1 to 4096 keys: 125 / 116 / 105 / 107 / 120 us for 512 / 1024 / 2048 / 4096 /
     // 8192), and no more than 64 ranges to join where 512 blocks have them
     const size_t left = ws_bytes - stage_bytes(p.tiles, D);
-    const int64_t pairs = B * Hk, full = 512 / pairs, want = (rows_tuning.blocks + pairs - 1) / pairs;
+    const int64_t pairs = B * Hk, full = 512 / pairs, want = (tuning.blocks + pairs - 1) / pairs;
     int64_t ranges = want > 64 && want > full ? (full > 64 ? full : 64) : want;
-    const int64_t least = rows_tuning.least * pairs < 2048 ? rows_tuning.least * pairs : 2048;
+    const int64_t least = tuning.least * pairs < 2048 ? tuning.least * pairs : 2048;
     if (least && ranges > max_len / least) ranges = max_len / least > 1 ? max_len / least : 1;
-    split_keys(p.rows, ranges, rows_tuning.unit, max_len, D, left);
+    split_keys(p.rows, ranges, tuning.unit, max_len, D, left);
   }
   return p;
 }

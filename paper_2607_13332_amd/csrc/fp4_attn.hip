@@ -7,8 +7,8 @@
 // pass over the keys with the running maximum m and sum l of the softmax: for a
 // tile of scores s, m' = max(m, max s), and with a = exp(m - m'), l' = a l + sum
 // exp(s - m'), O' = a O + sum exp(s - m') v; at the end O / l.
-#include "attn_plan.h"
 #include "fp4.h"
+#include "fp4_plan.h"
 
 namespace ssn {
 
@@ -92,24 +92,11 @@ __global__ __launch_bounds__(256) void paged_attn_fp4_generic(Fp4AttnArgs fa) {
   }
 }
 
-// How a call is run: attn_plan.h.
-// Rows kernel: a block's four waves take 128 keys at a time, and a range of fewer than
-// 256 is mostly the wait for its first.  64 single tokens over caches of 1 to 4096
-// keys (8 heads of 128) take 47 / 43 / 43 / 43 us for 512 / 1024 / 1536 / 2048 blocks,
-// 16 over up to 8192 32 / 26 / 30 / 31.  Ranges cost their join, 4 us and more, which
-// shorter ones do not give back where the pairs fill the chip by themselves: 64
-// sequences of up to 512 / 1024 / 2048 / 4096 keys take 12 / 16 / 27 / 48 us with one
-// range each and 20 / 24 / 33 / 44 with ranges for 1024 blocks.
-//
-// Beside the rows' blocks tiles do not need the whole chip: 517 tokens and 31 single
-// ones over up to 8192 keys take 150 / 121 / 125 us with 256 / 384 / 512 blocks, 256
-// tokens and 63 over up to 4096 87 / 90 / 97, 200 tokens and 15 over up to 32768 195 /
-// 195 / 207.
-constexpr RowsTuning kFp4Rows = {1024, 256, 4, 384};
+// How a call is run: fp4_plan.h.
 size_t fp4_attention_workspace_bytes(int dtype, int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D,
                                      int64_t max_q, int64_t max_len) {
   if (D > 256) return 0;
-  const AttnPlan p = attention_plan(dtype, N, B, Hq, Hk, D, max_q, max_len, (size_t)1 << 60, kFp4Rows);
+  const AttnPlan p = attention_plan(dtype, N, B, Hq, Hk, D, max_q, max_len, (size_t)1 << 60, kFp4Tuning);
   return stage_bytes(p.tiles, D) + stage_bytes(p.rows, D);
 }
 
@@ -131,7 +118,7 @@ hipError_t launch_paged_attention_fp4(int dtype, const Fp4AttnArgs& f, void* ws,
       hipLaunchKernelGGL((paged_attn_fp4_generic<float>), dim3(grid), dim3(256), 0, st, f);
     return hipGetLastError();
   }
-  AttnPlan p = attention_plan(dtype, a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0, kFp4Rows);
+  AttnPlan p = attention_plan(dtype, a.pb.N, a.pb.B, a.Hq, a.Hk, a.D, a.max_q, a.pb.max_len, ws ? ws_bytes : 0, kFp4Tuning);
   char* at = (char*)ws;
   for (AttnPart* x : {&p.tiles, &p.rows})
     if (const size_t bytes = stage_bytes(*x, a.D)) {

@@ -127,7 +127,15 @@ __device__ __forceinline__ void fp4_tiles_block(const Fp4AttnArgs& fa, const Att
     if (t + 2 < t1) fetch();
     if (t + 3 < t1) find(t + 3);
   };
-  constexpr bool kFirst = QB == 3;
+  // The widest tiles, and those of narrow heads, ask for the matrix cores first
+  // (s_setprio), so that of a SIMD's two waves one multiplies while the other
+  // exponentiates: 177 -> 162 us for a prompt of 4096 tokens (40 / 8 heads of 128), 92
+  // -> 89 with 32 / 8 heads of 64; 128 rows of heads of 128 lose 5 %, heads of 256 20.
+  constexpr bool kFirst = QB == 3 || (QB == 2 && DT == 64);
+  // Where a tile's scores are held at once its next codes go to LDS after its products
+  // (2048 tokens, 8 / 2 heads of 256: 78 -> 71 us), else before (4096 tokens of heads
+  // of 128: 162 us, 167 after the first half's products).
+  constexpr bool kLate = TK == SK;
   auto scores = [&](const char* kl, f32x4 (&s)[NKB][QB]) {
 #pragma unroll
     for (int k = 0; k < NKB; ++k) {
@@ -149,7 +157,7 @@ __device__ __forceinline__ void fp4_tiles_block(const Fp4AttnArgs& fa, const Att
   for (; t < t_open; ++t) {
     __syncthreads();
     const char *kl = lds[(t - t0) & 1][0], *vl = lds[(t - t0) & 1][1];
-    stage(t);
+    if constexpr (!kLate) stage(t);
 #pragma unroll
     for (int u = 0; u < TK; u += SK) {
       f32x4 s[NKB][QB];
@@ -162,6 +170,7 @@ __device__ __forceinline__ void fp4_tiles_block(const Fp4AttnArgs& fa, const Att
       weigh<Tag, RB, false>(vl + u * RB, vb, p, rs, odd);
       if constexpr (kFirst) __builtin_amdgcn_s_setprio(0);
     }
+    if constexpr (kLate) stage(t);
   }
   for (; t < t1; ++t) {
     __syncthreads();

@@ -115,3 +115,28 @@ def test_validation_is_clean_under_asan_and_ubsan(tmp_path):
     assert r.returncode == 0, (r.stdout + r.stderr)[-3000:]
     assert "4-bit cache validation ok" in r.stdout
     assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr
+
+
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir("/opt/rocm/include"),
+                    reason="needs g++ and the HIP headers")
+def test_plans_fit_every_size(tmp_path):
+    exe = str(tmp_path / "fp4_plan")
+    cmd = ["g++", "-std=c++17", "-O2", "-g", "-fsanitize=undefined", "-fno-sanitize-recover=all",
+           "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I" + os.path.join(ROOT, "paper_2607_13332_amd", "csrc"),
+           os.path.join(ROOT, "tests", "asan", "fp4_plan_driver.cpp"), "-o", exe]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-3000:]
+    assert "4-bit cache plans ok" in r.stdout
+
+
+def test_workspace_sizes(lib):
+    """Multiples of 16 bytes, and some where a long cache has few rows."""
+    f = lib.ssn_paged_attention_fp4_workspace_bytes
+    for dtype in (0, 1):
+        for D in (32, 64, 96, 128, 256):
+            for B, chunk, length in ((1, 1, 131072), (3, 1, 5000), (1, 512, 32768), (16, 200, 8000)):
+                need = f(dtype, B - 1 + chunk, B, 8, 2, D, chunk, length)
+                assert need % 16 == 0 and need < 1 << 33
+            assert f(dtype, 1, 1, 8, 2, D, 1, 131072) > 0
