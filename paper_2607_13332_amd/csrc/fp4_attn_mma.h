@@ -81,17 +81,15 @@ __device__ __forceinline__ void add_nan_groups(const uint8_t* scales, int D, con
 }
 
 // The row of LDS that holds key l of 16's values: rows of 8 consecutive keys take a
-// chunk each to different columns of 16 bytes (swizzle_values), and those of the 4
-// keys that a transposing read takes a piece of 32 bytes.
-template <int RB>
-__device__ __forceinline__ int value_row(int l) {
-  if constexpr (RB >= 256) return (l & 3) | ((l & 4) << 1) | ((l & 8) >> 1);
-  else return ((l & 7) << 1) | (l >> 3);
-}
+// chunk each to different columns (swizzle_values), and a transposing read, which is
+// served 256 bytes at a time, finds the pieces of 8 consecutive keys in different ones
+// too.  (With rows 0-3, 8-11, 4-7, 12-15 it does not: 25 % of the tile kernel's LDS
+// cycles were conflicts.)
+__device__ __forceinline__ int value_row(int l) { return l ^ ((l & 4) << 1); }
 // Mma::vbase() with the keys in these rows.
 template <int RB>
 __device__ __forceinline__ uint32_t value_base(int lane) {
-  const int L = lane & 15, row = value_row<RB>(4 * (lane >> 4) + (L >> 2));
+  const int L = lane & 15, row = value_row(4 * (lane >> 4) + (L >> 2));
   return row * RB + ((((uint32_t)(L & 3) >> 1) ^ swizzle_values<RB>(row)) << 4) + (L & 1) * 8;
 }
 

@@ -156,7 +156,7 @@ __device__ __forceinline__ void fp4_rows_block(const Fp4AttnArgs& fa, const Attn
       if (EXACT || e0 + 32 * i < D) s[i] = scales[at_s[k] + i];
     }
   };
-  const int v_row = value_row<RB>(lane & 15);
+  const int v_row = value_row(lane & 15);
   uint32_t vb[1] = {value_base<RB>(lane)}, vw = v_row * RB + (((uint32_t)(g * NC) ^ swizzle_values<RB>(v_row)) << 4);
 
   int t = k_begin + wave * TK;

@@ -71,7 +71,7 @@ __device__ __forceinline__ void fp4_tiles_block(const Fp4AttnArgs& fa, const Att
   // This thread's key of a tile, and the unit of its codes.  Keys past the last
   // repeat it (their scores are masked).
   const int unit = lane / KPW, e0 = unit * UE, key = wave * KPW + (lane & (KPW - 1));
-  const int v_row = (key & ~15) + value_row<RB>(key & 15);
+  const int v_row = (key & ~15) + value_row(key & 15);
   typedef uint32_t piece __attribute__((ext_vector_type(UW)));
   piece kreg = {}, vreg = {};
   uint32_t ks = 0, vs = 0;
