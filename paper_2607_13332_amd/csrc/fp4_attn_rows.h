@@ -1,6 +1,24 @@
 // Attention of few rows over a 4-bit cache: a block of 4 waves owns a range of the
-// keys of one sequence and key head; its waves take the range's tiles of 64 keys in
+// keys of one sequence and key head; its waves take the range's tiles of 32 keys in
 // turn, all with the same 16 QB rows, and join their results in LDS at the end.
+//
+// Keys are A operands as they come: a lane's 16 bytes are one group of its key, and a
+// product takes the elements 8 ch .. 8 ch + 7 of every lane's group, which the queries
+// are ordered to match.  Values become bf16 on their way to the wave's part of LDS and
+// are read transposed.  A lane has the same key of both, so that their addresses are
+// worked out once.
+//
+// What bounds it: memory, and for short caches the waits at a block's beginning and end.
+// 64 single tokens over caches of 1 to 4096 keys (8 heads of 128) take 37 us (3.9 TB/s)
+// and their join 6, four over 100000 to 131072 100 (5.6 TB/s; a large copy moves 5.1)
+// and 8; with the loads alone, nothing computed, 36 and 88.  The vector units issue
+// half of the time, the matrix cores a fifth; registers for four blocks of a compute
+// unit instead of three gain nothing.  Kept on the way, the two times in sum: as first
+// built 56 / 132; loads without a condition, tiles of 32 keys and three blocks 44 / 109;
+// one address for keys and values, queries in LDS, one exchange at the end 43 / 108.
+//
+// Probabilities go in the parts of attn_rows.h: two for bf16 (2^-16 of each), three for
+// float32 (all its bits).
 #pragma once
 
 #include "attn_rows.h"
