@@ -657,7 +657,9 @@ ssn_status_t ssn_kv_read_fp4(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hk
  * ssn_paged_attention_fp4 -- ssn_paged_attention over a 4-bit cache, with K_t and
  * V_t the values that it stands for (they are exact in bf16, so keys and values
  * are not rounded again).  dtype is that of Q and O; the other arguments, the
- * rounding of probabilities in bf16 and what a row does not see are as there.
+ * rounding of probabilities in bf16 and what a row does not see are as there.  Groups
+ * with s of 253 and 254, which reach infinity and which appends do not write, may count
+ * as NaN.
  */
 size_t ssn_paged_attention_fp4_workspace_bytes(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq,
                                                int64_t Hk, int64_t D, int64_t max_q,

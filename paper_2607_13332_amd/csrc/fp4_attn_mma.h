@@ -26,7 +26,9 @@ struct Mma<OverFp4<T>> : Mma<uint16_t> {
                          (s[i >> 1][2 * (i & 1) + 1] - hi_bf16(p[i])) - hi_bf16(r[i]));
     return l;
   }
-  // (the cache has no infinities, and a NaN is one whatever it is multiplied with)
+  // (infinities, of scale bytes that appends do not write, may become NaN against a
+  // second part that is zero or of the other sign: 64 single tokens take 48 us instead
+  // of 44 with them bounded, four long ones 123 instead of 109)
   __device__ static __forceinline__ u32x4 bounded(u32x4 v) { return v; }
 };
 
@@ -65,14 +67,15 @@ struct QueryChunk {
   }
 };
 
-// The NaN that weigh<MASKED> left out of row `scales` of V's scales, for the rows
-// of O that see it.
+// What weigh<MASKED> left out of a row of V with these scales, for the rows of O that
+// see it: groups of NaN, and those that may hold infinities count as such.
+constexpr int kNotFinite = 253;        // from this scale byte on
 template <int DT16, int QB>
-__device__ __forceinline__ void add_nan_groups(const uint8_t* scales, int D, const bool (&sees)[QB],
+__device__ __forceinline__ void add_not_finite_groups(const uint8_t* scales, int D, const bool (&sees)[QB],
                                                RowState<DT16, QB>& st) {
 #pragma unroll
   for (int d = 0; d < DT16; ++d)
-    if (16 * d < D && scales[d / 2] == kNanScale) {
+    if (16 * d < D && scales[d / 2] >= kNotFinite) {
 #pragma unroll
       for (int q = 0; q < QB; ++q)
 #pragma unroll

@@ -251,7 +251,7 @@ __device__ __forceinline__ void fp4_rows_block(const Fp4AttnArgs& fa, const Attn
           *(u32x4*)(vl + 16 * (k & 1) * RB + (vw ^ (uint32_t)(ch << 4))) =
               fp4_bf16x8(vreg[k][ch], fp4_scale(vs[k][8 * ch / kFp4Group]));
         load(a.Vc, fa.Vs, k, vreg[k], vs[k]);
-          }
+      }
       wave_lds_order();
       u32x4 ph[PARTS][1][QB];
 #pragma unroll
@@ -271,7 +271,7 @@ __device__ __forceinline__ void fp4_rows_block(const Fp4AttnArgs& fa, const Attn
         bool sees[QB];
 #pragma unroll
         for (int q = 0; q < QB; ++q) sees[q] = u <= seen[q];
-        add_nan_groups(fa.Vs + (int64_t)cache_row(a.pb, b, a.Hk, kh, u) * groups, a.D, sees, rs);
+        add_not_finite_groups(fa.Vs + (int64_t)cache_row(a.pb, b, a.Hk, kh, u) * groups, a.D, sees, rs);
       }
   }
   fp4_finish<T, DT, QB, EXACT>(a, part, rs, lds, seen, rows, sq.s0, kh, range, ((int64_t)b * a.Hk + kh) * (16 * QB),

@@ -215,7 +215,7 @@ __device__ __forceinline__ void fp4_tiles_block(const Fp4AttnArgs& fa, const Att
       bool sees[QB];
 #pragma unroll
       for (int q = 0; q < QB; ++q) sees[q] = k <= seen[q];
-      add_nan_groups(fa.Vs + (int64_t)cache_row(a.pb, b, a.Hk, kh, k) * groups, a.D, sees, rs);
+      add_not_finite_groups(fa.Vs + (int64_t)cache_row(a.pb, b, a.Hk, kh, k) * groups, a.D, sees, rs);
     }
   }
   finish_rows<T, DT, QB, EXACT>(a, part, rs, row, seen, rows, sq.s0, kh, range, -1, ranges == 1, c, lane);

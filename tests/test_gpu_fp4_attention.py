@@ -117,6 +117,65 @@ def test_a_group_without_values_stays_in_its_place(dtype, new, D):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 4, 70, 200])
+@pytest.mark.parametrize("D", [64, 96, 128, 256, 320])
+def test_values_past_the_range_of_bf16(dtype, new, D):
+    """Scale bytes 253 and 254, which appends do not write: 6 2^126 and 2^128 are
+    infinite.  A value like that makes one element of the rows that see it infinite,
+    with its sign, or NaN, and may make the rest of its group NaN; other elements keep
+    their bits, and so do rows before it."""
+    Hq, Hk, length = 4, 2, 700
+    bt = Fp4Batch([(new, length)], Hk, D, 16, 3)
+    page, off = bt.slots(0)
+    for at in (40, length - new, length - 1 - new // 2, length - 1):
+        for c, byte, code in ((0, 253, 7), (17, 253, 15), (1, 254, 12), (31, 254, 4)):
+            where = page[at], 1, off[at]
+            bt.held[2][where][16:32] = 0
+            bt.held[3][where][1] = byte
+            q, clean, _ = attend(bt, Hq, Hk, D, dtype, 2)
+            bt.held[2][where][16 + c // 2] = code << (4 * (c % 2))
+            _, out, _ = attend(bt, Hq, Hk, D, dtype, 2, q=q)
+            got, want = f64(out), np.array(f64(clean))
+            see = slice(max(0, at - (length - new)), None), slice(2, None), 32 + c
+            assert (np.isnan(got[see]) | (got[see] == (-np.inf if code > 7 else np.inf))).all(), (at, byte, code)
+            got[see] = want[see] = 0
+            nan = np.isnan(got)
+            assert not nan[:see[0].start].any() and not nan[:, :2].any() and not np.delete(nan, np.s_[32:64], -1).any()
+            assert np.array_equal(np.where(nan, 0, got), np.where(nan, 0, want)), (at, byte, code)
+            bt.held[2][where][16 + c // 2] = bt.held[3][where][1] = 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 4, 70])
+@pytest.mark.parametrize("D", [64, 128, 256, 320])
+def test_keys_past_the_range_of_bf16(dtype, new, D):
+    """A key element of -2^128, under queries that are positive there: the heads that
+    see it have no weight for it, as for a finite one of -2^74, or are NaN; the others
+    keep their bits, and so do rows before it."""
+    Hq, Hk, length = 4, 2, 700
+    bt = Fp4Batch([(new, length)], Hk, D, 16, 3)
+    page, off = bt.slots(0)
+    q = np.array(f64(normal(np.random.default_rng(2), (new, Hq, D), dtype, 1.5)))
+    q[:, :, 3] = np.abs(q[:, :, 3]) + 0.5
+    q = I.store(q, dtype)
+    for at in (40, length - 1 - new // 2):
+        where = page[at], 1, off[at]
+        bt.held[0][where][:] = 0
+        bt.held[0][where][1] = 0xC0                    # element 3: -2
+        bt.held[1][where][0] = 200
+        _, clean, _ = attend(bt, Hq, Hk, D, dtype, 2, q=q)
+        assert np.isfinite(f64(clean)).all()
+        bt.held[1][where][0] = 254
+        _, out, _ = attend(bt, Hq, Hk, D, dtype, 2, q=q)
+        got, want = f64(out), np.array(f64(clean))
+        see = slice(max(0, at - (length - new)), None), slice(2, None)
+        bad = np.isnan(got[see]).all(-1)
+        got[see][bad] = want[see][bad] = 0
+        assert np.array_equal(got, want), at
+        bt.held[1][where][0] = 200
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 4.0])
 def test_scales_and_far_scores(dtype, scale):
     """Scores far apart (scale 4: hundreds), equal ones, a negative scale."""
