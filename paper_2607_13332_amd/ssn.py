@@ -192,6 +192,17 @@ def _stream(stream) -> int:
     return int(stream.cuda_stream)
 
 
+def _stream_on(stream, dev: int) -> int:
+    """_stream, of the GPU `dev` that the call's tensors are on: a kernel
+    launched on another would read and write memory that it may not reach.  A
+    default stream has the handle 0, which is the current device's."""
+    if stream is not None and getattr(stream, "device_index", dev) != dev:
+        raise ValueError(f"tensors are on GPU {dev}, the stream is on GPU {stream.device_index}")
+    if (stream is None or not stream.cuda_stream) and dev != _get_device():
+        raise ValueError(f"tensors are on GPU {dev}, the current device is {_get_device()}: make theirs the current one")
+    return _stream(stream)
+
+
 def _dev(t: torch.Tensor, name: str, dtype=None, ndim=None):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -881,6 +892,8 @@ def paged_attention(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, pages: 
 # [pages, Hk, page_size, D / 32], uint8, for keys and for values; D a multiple
 # of 32.  32 consecutive elements share a power of two 2^(s - 127) and each is the
 # nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it, with its sign.
+# A call's tensors are on the device of its stream, or of the current one; others are
+# refused (0.1 us of a call).
 # --------------------------------------------------------------------------
 FP4_GROUP = 32
 
@@ -947,7 +960,7 @@ def kv_append_fp4(K: torch.Tensor, V: torch.Tensor, Kc: torch.Tensor, Ks: torch.
         _code(t), N, B, Hq, Hk, D, R, P, code, e, *q, *_rows(K, "K", K, g, t, N, Hk, D),
         *_rows(V, "V", K, g, t, N, Hk, D), _weight(wq, "wq", K, g, t, D) if Hq else None,
         _weight(wk, "wk", K, g, t, D), _gpu(table, "table", K, g, torch.float32, 2) if R else None,
-        *paged, *qo, _stream(stream)))
+        *paged, *qo, _stream_on(stream, g)))
     return Qout if Q is not None else None
 
 
@@ -969,7 +982,7 @@ def kv_read_fp4(Kc: torch.Tensor, Ks: torch.Tensor, Vc: torch.Tensor, Vs: torch.
     B, paged = _paged_fp4(Kc, Ks, Vc, Vs, pages, starts, lens, Kc, g, Hk, D)
     _check("ssn_kv_read_fp4", lib().ssn_kv_read_fp4(
         _code(dtype), N, B, Hk, D, *paged, *_rows(Kout, "Kout", Kc, g, dtype, N, Hk, D),
-        *_rows(Vout, "Vout", Kc, g, dtype, N, Hk, D), _stream(stream)))
+        *_rows(Vout, "Vout", Kc, g, dtype, N, Hk, D), _stream_on(stream, g)))
     return Kout, Vout
 
 
@@ -1007,5 +1020,5 @@ def paged_attention_fp4(Q: torch.Tensor, Kc: torch.Tensor, Ks: torch.Tensor, Vc:
         *_rows(Q, "Q", Q, g, t, N, Hq, D), *paged, *_rows(out, "out", Q, g, t, N, Hq, D),
         None if lse is None else _gpu(lse, "lse", Q, g, torch.float32, 2),
         None if workspace is None else _gpu(workspace, "workspace", Q, g, torch.uint8, 1),
-        0 if workspace is None else workspace.numel(), _stream(stream)))
+        0 if workspace is None else workspace.numel(), _stream_on(stream, g)))
     return out
