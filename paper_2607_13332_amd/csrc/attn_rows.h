@@ -29,49 +29,13 @@ constexpr int rows_lds() {
   return (tiles > join ? tiles : join) + 4 * QB * kWave * 4;         // and m, l of two waves
 }
 
-// The results of a block's waves, whose rows are the same, into wave 0's; at the
-// end of `bytes` of LDS lie m and l of two waves.
-template <int DT16, int QB>
-__device__ __forceinline__ void join_waves(RowState<DT16, QB>& rs, char* lds, int bytes, int wave, int lane, float c) {
-  constexpr int kJoin = DT16 * QB * kWave * 16;
-  float(*joint)[2][QB][kWave] = (float(*)[2][QB][kWave])(lds + bytes - 4 * QB * kWave * 4);
-  // 2 and 3 into 0 and 1, then 1 into 0.
-#pragma unroll
-  for (int step = 2; step >= 1; step >>= 1) {
-    __syncthreads();
-    if (wave >= step && wave < 2 * step) {
-#pragma unroll
-      for (int q = 0; q < QB; ++q) {
-        joint[wave - step][0][q][lane] = rs.m[q];
-        joint[wave - step][1][q][lane] = rs.l[q];
-#pragma unroll
-        for (int d = 0; d < DT16; ++d)
-          *(f32x4*)(lds + (wave - step) * kJoin + ((d * QB + q) * kWave + lane) * 16) = rs.o[d][q];
-      }
-    }
-    __syncthreads();
-    if (wave < step) {
-#pragma unroll
-      for (int q = 0; q < QB; ++q) {
-        const float m2 = joint[wave][0][q][lane], l2 = joint[wave][1][q][lane];
-        const float m = fmaxf(rs.m[q], m2), base = m == kNegInf ? 0.f : m;
-        const float w1 = __builtin_amdgcn_exp2f((rs.m[q] - base) * c), w2 = __builtin_amdgcn_exp2f((m2 - base) * c);
-        rs.m[q] = m;
-        rs.l[q] = rs.l[q] * w1 + l2 * w2;
-#pragma unroll
-        for (int d = 0; d < DT16; ++d)
-          rs.o[d][q] = rs.o[d][q] * w1 + *(const f32x4*)(lds + wave * kJoin + ((d * QB + q) * kWave + lane) * 16) * w2;
-      }
-    }
-  }
-}
-
 template <typename T, int DT, int QB, bool EXACT>
 __device__ __forceinline__ void rows_block(const AttnArgs& a, const AttnPart& part, int few, int id, char* lds) {
   using M = Mma<T>;
   constexpr int RB = DT * (int)sizeof(T), TK = M::kKeys, NKB = TK / 16, NC = RB / 64, DT16 = DT / 16;
   constexpr int CH = RB / 16, RPI = kWave / CH, NI = TK / RPI;
-  constexpr int kTile = TK * RB;
+  constexpr int kTile = TK * RB, kJoin = rows_join<T, DT, QB>();
+  float(*joint)[2][QB][kWave] = (float(*)[2][QB][kWave])(lds + rows_lds<T, DT, QB>() - 4 * QB * kWave * 4);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kh = id % a.Hk, rest = id / a.Hk, b = rest % a.pb.B, range = rest / a.pb.B;
   const Sequence sq = sequence_of(a.pb, b);
@@ -191,7 +155,35 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, const AttnPart& pa
       }
   }
 
-  join_waves<DT / 16, QB>(rs, lds, rows_lds<T, DT, QB>(), wave, lane, c);
+  // Join the waves: 2 and 3 into 0 and 1, then 1 into 0.
+#pragma unroll
+  for (int step = 2; step >= 1; step >>= 1) {
+    __syncthreads();
+    if (wave >= step && wave < 2 * step) {
+#pragma unroll
+      for (int q = 0; q < QB; ++q) {
+        joint[wave - step][0][q][lane] = rs.m[q];
+        joint[wave - step][1][q][lane] = rs.l[q];
+#pragma unroll
+        for (int d = 0; d < DT16; ++d)
+          *(f32x4*)(lds + (wave - step) * kJoin + ((d * QB + q) * kWave + lane) * 16) = rs.o[d][q];
+      }
+    }
+    __syncthreads();
+    if (wave < step) {
+#pragma unroll
+      for (int q = 0; q < QB; ++q) {
+        const float m2 = joint[wave][0][q][lane], l2 = joint[wave][1][q][lane];
+        const float m = fmaxf(rs.m[q], m2), base = m == kNegInf ? 0.f : m;
+        const float w1 = __builtin_amdgcn_exp2f((rs.m[q] - base) * c), w2 = __builtin_amdgcn_exp2f((m2 - base) * c);
+        rs.m[q] = m;
+        rs.l[q] = rs.l[q] * w1 + l2 * w2;
+#pragma unroll
+        for (int d = 0; d < DT16; ++d)
+          rs.o[d][q] = rs.o[d][q] * w1 + *(const f32x4*)(lds + wave * kJoin + ((d * QB + q) * kWave + lane) * 16) * w2;
+      }
+    }
+  }
   if (wave == 0)
     finish_rows<T, DT, QB, EXACT>(a, part, rs, row, seen, rows, sq.s0, kh, range,
                                   ((int64_t)b * a.Hk + kh) * (16 * QB), ranges == 1, c, lane);
