@@ -659,7 +659,8 @@ ssn_status_t ssn_kv_read_fp4(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hk
  * are not rounded again).  dtype is that of Q and O; the other arguments, the
  * rounding of probabilities in bf16 and what a row does not see are as there.  Groups
  * with s of 253 and 254, which reach infinity and which appends do not write, may count
- * as NaN.
+ * as NaN.  O is summed in float32 before it is divided by the probabilities' sum: it is
+ * finite where |V_t| is below 2^118 over the number of keys that a row sees.
  */
 size_t ssn_paged_attention_fp4_workspace_bytes(ssn_dtype_t dtype, int64_t N, int64_t B, int64_t Hq,
                                                int64_t Hk, int64_t D, int64_t max_q,
