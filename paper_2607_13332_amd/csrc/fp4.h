@@ -4,8 +4,9 @@
 // an element is a sign, two bits of exponent and one of fraction:
 //   code & 7    0   1    2   3    4   5   6   7
 //   level       0  0.5   1  1.5   2   3   4   6
-// A level is exact in bf16 at any scale (two significant bits), so that attention
-// multiplies what the cache stands for, with no further rounding.
+// A level is exact in bf16 at every scale that appends write (two significant bits;
+// under s of 253 and 254 the larger levels are infinite), so that attention multiplies
+// what the cache stands for, with no further rounding.
 #pragma once
 
 #include "attn_device.h"

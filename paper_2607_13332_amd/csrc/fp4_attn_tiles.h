@@ -14,7 +14,11 @@
 // exponentials (195 us, 218 without the turns).
 //
 // bf16 probabilities are rounded once for the product with V (2^-8 of each at most), as
-// over a bf16 cache; float32 ones go in three parts, against one of K and V: prompts of
+// over a bf16 cache.  What the rounding leaves as a second product, as the rows kernel
+// has it: prompts of 300 / 1024 / 2048 / 4096 tokens take 19 / 29 / 69 / 218 us with it
+// and 18.5 / 26 / 55 / 160 without, 512 tokens over 32768 keys 382 and 279, 517 beside 31
+// single ones 145 and 119.  The outputs' error against float64 is 0.0022 to 0.0023, 0.0016
+// with it, which is their own rounding.  Float32 ones go in three parts, against one of K and V: prompts of
 // 300 to 1024 tokens (16 heads of 64) 31 us where float32 products over a float32 cache
 // take 70.
 #pragma once

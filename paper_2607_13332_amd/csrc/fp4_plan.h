@@ -23,7 +23,8 @@ namespace ssn {
 // (40 / 8 heads of 128) 27 / 32 / 48, 2048 77 / 57 / 75, 4096 252 / 179 / 162; of heads of
 // 64 (32 / 8) 2048 33 / 39, 4096 101 / 88.  Chunks at the end of much longer sequences
 // have their keys split to fill it: 64 tokens over 8000 keys 37 / 34 / 35, 256 80 / 75 /
-// 65, twice 512 over 6000 150 / 139 / 151.
+// 65, twice 512 over 6000 150 / 139 / 151 (the rule takes 192 rows there too: it does not
+// look at how many of the chip's places a width leaves empty).
 inline int fp4_tile_rows(int dtype, int64_t rows, int64_t most, int64_t max_q, int64_t Hk, int64_t D,
                          int64_t max_len) {
   if (dtype != kBF16 || D > 128 || most <= 64) return 1;
